@@ -1,0 +1,1142 @@
+// Attention over the pages of a cache.
+//
+// With z_j = scale * log2(e) * q . k_j over the keys a query sees, one pass
+// keeps a running reference m, l = sum_j 2^(z_j - m) and o = sum_j 2^(z_j - m) v_j,
+// both multiplied by 2^(m - m') whenever m grows to m'; the result is o / l.
+// Parts over different keys join the same way.  In an 8-bit cache with scales
+// s_j (keys) and t_j (values), z_j has s_j as a factor, and the weight of the
+// value's code is 2^(z_j - m) t_j: m runs over z_j + log2 t_j, which keeps these
+// weights within (0, 1], where the 16-bit floats are densest.
+//
+// Matrix instructions compute S^T = K Q^T and O^T = V^T P^T.  S^T leaves a
+// query's scores in one lane column, four neighbouring keys in a lane, and that
+// is the layout in which the next product takes P^T if its sum over keys is
+// taken in the order (lane group, register); so weights never leave their lane.
+// V^T comes from shared memory by transposing reads.
+#include <algorithm>
+#include <cmath>
+
+#include "kv_common.h"
+
+namespace {
+
+using namespace kv;
+
+struct Args {
+  const uint16_t *q;
+  int64_t qt, qh;
+  uint16_t *out;
+  int64_t ot, oh;
+  float *lse;
+  const char *k, *v;
+  const float *ks, *vs;
+  const int32_t *table;
+  int64_t table_stride;
+  int32_t capacity;  // keys that the table's columns hold
+  const int32_t *starts, *lens;
+  int32_t n_seq, n_tokens;
+  int32_t heads, kv_heads, group;
+  int32_t pages, page_shift;
+  float scale;  // times log2(e)
+  int32_t causal, window;
+  int32_t q_bf16;
+  // results of parts, the sums o and (m, l): few rows [request][KV head][16]
+  // [part], many rows [token][head][part]
+  float *few_o, *many_o;
+  float2 *few_ml, *many_ml;
+  int32_t few_splits, few_chunk;    // of a few-rows launch: parts, keys a part
+  int32_t many_splits, many_chunk;  // of a many-rows launch
+  int32_t both;          // requests of more than 16 rows are the other launch's
+  int32_t row_blocks;
+};
+
+constexpr int kFewRows = 16;
+
+// The queries of request b and its keys.
+struct Seq {
+  int32_t q0, n, m;
+};
+__device__ __forceinline__ Seq get_seq(const Args &a, int32_t b) {
+  Seq s;
+  s.q0 = min(max(a.starts[b], 0), a.n_tokens);
+  s.n = min(max(a.starts[b + 1], s.q0), a.n_tokens) - s.q0;
+  s.m = max(a.lens[b], 0);
+  return s;
+}
+
+// Keys [lo, hi) that token i of the request sees.
+struct Range {
+  int32_t lo, hi;
+};
+__device__ __forceinline__ Range token_range(const Args &a, const Seq &s, int32_t i) {
+  Range r;
+  const int32_t p = s.m - s.n + i;
+  r.hi = min(s.m, a.capacity);
+  if (a.causal) r.hi = max(min(r.hi, p + 1), 0);
+  r.lo = a.window ? max(p - a.window + 1, 0) : 0;
+  r.lo = min(r.lo, r.hi);
+  return r;
+}
+
+// Keys of the rows r0 .. r1 (inclusive): the first token's first to the last
+// token's last, from a multiple of `unit` on.
+__device__ __forceinline__ Range block_range(const Args &a, const Seq &s, int32_t r0, int32_t r1,
+                                             int32_t unit) {
+  Range first = token_range(a, s, r0 / a.group), last = token_range(a, s, r1 / a.group);
+  Range r;
+  r.hi = last.hi;
+  r.lo = min(first.lo, r.hi) / unit * unit;
+  return r;
+}
+
+__device__ __forceinline__ int32_t parts_of(Range r, int32_t chunk, int32_t splits) {
+  return max(1, min(splits, (r.hi - r.lo + chunk - 1) / chunk));
+}
+
+// The parts of a few-rows block.  A request that has more rows than its launch
+// was laid out for has no room for parts.
+__device__ __forceinline__ int32_t few_parts(const Args &a, Range r, int32_t rows) {
+  return rows > kFewRows ? 1 : parts_of(r, a.few_chunk, a.few_splits);
+}
+
+// Key j of a request, 0 < end: its page's entry in the table, read ahead (the
+// last key's behind the end), and the row of the cache that it has for KV head h.
+__device__ __forceinline__ int32_t page_entry(const Args &a, int32_t b, int32_t j, int32_t end) {
+  return a.table[b * a.table_stride + (min(j, end - 1) >> a.page_shift)];
+}
+__device__ __forceinline__ int32_t cache_row(const Args &a, int32_t page, int32_t h, int32_t j,
+                                             int32_t end) {
+  if (j >= end || (uint32_t)page >= (uint32_t)a.pages) return kNoRow;
+  return ((page * a.kv_heads + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+}
+
+template <bool BF>
+__device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, x),
+                                                   __builtin_bit_cast(bf8v, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, x),
+                                                  __builtin_bit_cast(half8, y), c, 0, 0, 0);
+}
+template <bool BF>
+__device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, x),
+                                                   __builtin_bit_cast(bf8v, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, x),
+                                                  __builtin_bit_cast(half8, y), c, 0, 0, 0);
+}
+
+template <bool BF>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  if constexpr (BF) {
+    const bf2v p = {(__bf16)x, (__bf16)y};
+    return __builtin_bit_cast(uint32_t, p);
+  } else {
+    const half2v p = {(_Float16)x, (_Float16)y};
+    return __builtin_bit_cast(uint32_t, p);
+  }
+}
+
+// Four 16-bit elements down a column of four rows: within 16 lanes, lane i
+// names row i / 4 and the columns 4 (i % 4) .. + 3 of a 4 x 16 tile and gets
+// column i.
+__device__ __forceinline__ u32x2 read_column(const char *p) {
+  using lds_short4 = __attribute__((address_space(3))) short4v;
+  short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)p);
+  return __builtin_bit_cast(u32x2, x);
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row of a bf16 query as halves times a power of two, 2^-e with 2^e the row's
+// largest magnitude's; what this loses lies 2^-25 and more below that.
+__device__ __forceinline__ int row_exponent(uint32_t top_bits) {
+  return min(max((int)(top_bits >> 23) - 127, -100), 126);
+}
+__device__ __forceinline__ u32x4 bf16_to_half(u32x4 x, float by) {
+  u32x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    y[i] = pack2<false>(__uint_as_float(x[i] << 16) * by, __uint_as_float(x[i] & 0xffff0000u) * by);
+  return y;
+}
+__device__ __forceinline__ uint32_t top_of(u32x4 x) {  // bf16 magnitudes, as fp32 bits
+  uint32_t t = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t = max(t, max((x[i] << 16) & 0x7fffffffu, x[i] & 0x7fff0000u));
+  return t;
+}
+
+// Values that are not finite must reach the rows that see them and no others,
+// and a weight of zero does not keep them out of a product.  So where some row
+// of a block does not see all of a tile, they go into the product as zeros, and
+// are added to the rows that see them after the loop (add_unbounded): the
+// result is an infinity or a NaN whatever the weight.
+template <bool BF>
+__device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {
+  constexpr uint32_t hi = BF ? 0x7f800000u : 0x7c000000u, lo = hi >> 16;
+  return ((w & hi) == hi ? 0xffff0000u : 0u) | ((w & lo) == lo ? 0xffffu : 0u);
+}
+template <bool BF>
+__device__ __forceinline__ bool take_unbounded(u32x4 &x) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = unbounded_mask<BF>(x[i]);
+    any |= m;
+    x[i] &= ~m;
+  }
+  return any != 0;
+}
+// Element d of a row of values, if it is not finite; otherwise zero.
+template <int TYPE, int D>
+__device__ __forceinline__ float unbounded_value(const Args &a, int32_t row, int d) {
+  float x;
+  if constexpr (TYPE == WS_KV_BF16)
+    x = Bf16::get(((const uint16_t *)a.v)[(int64_t)row * D + d]);
+  else if constexpr (TYPE == WS_KV_FP16)
+    x = Fp16::get(((const uint16_t *)a.v)[(int64_t)row * D + d]);
+  else
+    x = (((const uint8_t *)a.v)[(int64_t)row * D + d] & 0x7f) == 0x7f ? NAN : 0.0f;
+  return isfinite(x) ? 0.0f : x;
+}
+
+// o / l in the output's type; a query that sees nothing has l = 0.
+__device__ __forceinline__ float safe_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ uint16_t out_bits(const Args &a, float x) {
+  return a.q_bf16 ? Bf16::put(x) : Fp16::put(x);
+}
+__device__ __forceinline__ float natural_lse(float m, float l) {
+  return l == 0.0f ? -INFINITY : 0.69314718055994530942f * (m + log2f(l));
+}
+
+// ------------------------------------------------------- few rows -------
+//
+// Up to 16 rows (tokens x heads of a group) of a request and KV head: each
+// cached element is read once for all of them, so the cache's bytes bound this.
+// Four waves take 32 keys each in turn, with their own running sums, and join
+// at the end; long requests are split over workgroups too.  Keys go from memory
+// into the matrix layout directly; values by way of shared memory, 32 rows a
+// wave, for the transposing read.
+
+template <int TYPE>
+constexpr bool kBf = TYPE == WS_KV_BF16;
+template <int TYPE>
+constexpr bool kCodes = TYPE == WS_KV_FP8 || TYPE == WS_KV_INT8;
+
+template <int TYPE, int D>
+struct Few {
+  static constexpr int esz = kCodes<TYPE> ? 1 : 2;
+  static constexpr int steps = D / 32;            // of the product over d
+  static constexpr int tiles = D / 16;            // of the result
+  static constexpr int kloads = D * esz / 64;     // 16-byte loads of a key tile
+  static constexpr int chunks = D * esz / 16;     // 16-byte chunks of a row
+  static constexpr int vrows = 64 / chunks;       // rows of one value load
+  static constexpr int vloads = 32 / vrows;
+  static constexpr int row_bytes = D * 2;         // a row of values in shared memory
+  static constexpr int wave_bytes = 32 * row_bytes + 32 * 12;
+  static constexpr int join_stride = D + 4;       // floats
+  static constexpr int join_bytes = 4 * 16 * (join_stride + 2) * 4;
+  static constexpr int smem = wave_bytes * 4 > join_bytes ? wave_bytes * 4 : join_bytes;
+};
+
+// 16-byte chunk c of key row `key` lies at chunk c ^ few_swizzle(key), which
+// spreads the 8 rows that 32 lanes of a transposing read touch over the banks.
+template <int D>
+__device__ __forceinline__ int few_swizzle(int key) {
+  return D == 64 ? ((key >> 1) & 3) << 1 : (key & 7) << 1;
+}
+
+template <int TYPE, int D>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a) {
+  using F = Few<TYPE, D>;
+  constexpr bool BF = kBf<TYPE>;
+  constexpr bool CODES = kCodes<TYPE>;
+  __shared__ alignas(16) char smem[F::smem];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n16 = lane & 15, g = lane >> 4;
+  const int32_t split = blockIdx.x % a.few_splits;
+  const int32_t at = blockIdx.x / a.few_splits;
+  const int32_t h = at % a.kv_heads, b = at / a.kv_heads;
+  const Seq s = get_seq(a, b);
+  const int32_t rows = s.n * a.group;
+  if (a.both && rows > kFewRows) return;
+
+  char *vbuf = smem + wave * F::wave_bytes;
+  float *kscale = (float *)(vbuf + 32 * F::row_bytes), *vlog = kscale + 32, *vscale = vlog + 32;
+
+  for (int32_t r0 = 0; r0 < rows; r0 += kFewRows) {
+    const int32_t r1 = min(r0 + kFewRows, rows) - 1;
+    const Range block = block_range(a, s, r0, r1, 32);
+    const int32_t parts = few_parts(a, block, rows);
+    if (split >= parts) continue;
+    const int32_t begin = block.lo + split * a.few_chunk;
+    const int32_t end = split == parts - 1 ? block.hi : begin + a.few_chunk;
+    const int32_t row = r0 + n16;
+    const bool live = row <= r1;
+    const int32_t token = live ? row / a.group : 0;
+    const int32_t head = h * a.group + (live ? row - token * a.group : 0);
+    Range see = token_range(a, s, token);
+    if (!live) see = {0, 0};
+    // keys that every row of the block sees
+    const Range lo_all = token_range(a, s, r1 / a.group), hi_all = token_range(a, s, r0 / a.group);
+
+    // the queries, in the layout of the product
+    u32x4 q[F::steps];
+    float by = a.scale;
+    {
+      const uint16_t *p = a.q + (int64_t)(s.q0 + token) * a.qt + (int64_t)head * a.qh;
+      const bool wide = ((a.qt | a.qh) & 7) == 0 && ((uintptr_t)a.q & 15) == 0;
+#pragma unroll
+      for (int i = 0; i < F::steps; ++i) {
+        const int d = CODES ? 64 * (i / 2) + 16 * g + 8 * (i % 2) : 32 * i + 8 * g;
+        if (!live) {
+          q[i] = u32x4{0, 0, 0, 0};
+        } else if (wide) {
+          q[i] = *reinterpret_cast<const u32x4 *>(p + d);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            q[i][j] = (uint32_t)p[d + 2 * j] | (uint32_t)p[d + 2 * j + 1] << 16;
+        }
+      }
+      if (CODES && a.q_bf16) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < F::steps; ++i) top = max(top, top_of(q[i]));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const int e = row_exponent(top);
+#pragma unroll
+        for (int i = 0; i < F::steps; ++i) q[i] = bf16_to_half(q[i], ldexpf(1.0f, -e));
+        by *= ldexpf(1.0f, e);
+      }
+    }
+
+    f32x4 o[F::tiles];
+#pragma unroll
+    for (int i = 0; i < F::tiles; ++i) o[i] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+    bool bad = false;  // a value was taken out
+
+    u32x4 kreg[2][F::kloads], vreg[F::vloads];
+    float ks = 0.0f, vs = 0.0f;
+    auto load_keys = [&](int32_t at_row) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int64_t r = max(__shfl(at_row, 16 * t + n16), 0);
+        const char *p = a.k + r * (D * F::esz) + 16 * g;
+#pragma unroll
+        for (int i = 0; i < F::kloads; ++i)
+          kreg[t][i] = *reinterpret_cast<const u32x4 *>(p + 64 * i);
+      }
+      if constexpr (CODES) ks = a.ks[max(at_row, 0)];
+    };
+    auto load_values = [&](int32_t at_row) {
+#pragma unroll
+      for (int i = 0; i < F::vloads; ++i) {
+        const int64_t r = max(__shfl(at_row, i * F::vrows + lane / F::chunks), 0);
+        vreg[i] = *reinterpret_cast<const u32x4 *>(a.v + r * (D * F::esz) + 16 * (lane % F::chunks));
+      }
+      if constexpr (CODES) vs = a.vs[max(at_row, 0)];
+    };
+
+    int32_t k0 = begin + 32 * wave;
+    const int32_t mine = lane & 31;
+    int32_t row_at = kNoRow, next_page = 0;
+    if (k0 < end) {
+      const int32_t page = page_entry(a, b, k0 + mine, end);
+      next_page = page_entry(a, b, k0 + 128 + mine, end);
+      row_at = cache_row(a, page, h, k0 + mine, end);
+      load_keys(row_at);
+      load_values(row_at);
+    }
+    for (; k0 < end; k0 += 128) {
+      const bool more = k0 + 128 < end;
+      const int32_t next_at = cache_row(a, next_page, h, k0 + 128 + mine, end);
+      const uint32_t there = (uint32_t)__ballot(row_at != kNoRow);
+      if constexpr (CODES) {
+        if (lane < 32) {
+          kscale[lane] = ks;
+          // below 2^-110 the reference no longer follows, the weight still does
+          vlog[lane] = fmaxf(log2f(vs), -110.0f);
+          vscale[lane] = vs;
+        }
+      }
+      // scores: lane (n16, g) gets keys 16 t + 4 g + r of its row
+      f32x4 z[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        z[t] = f32x4{0, 0, 0, 0};
+        if constexpr (CODES) {
+#pragma unroll
+          for (int i = 0; i < F::kloads; ++i) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const u32x2 x = codes_to_half<TYPE>(kreg[t][i][2 * half]);
+              const u32x2 y = codes_to_half<TYPE>(kreg[t][i][2 * half + 1]);
+              z[t] = mfma16<false>(u32x4{x[0], x[1], y[0], y[1]}, q[2 * i + half], z[t]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < F::kloads; ++i) z[t] = mfma16<BF>(kreg[t][i], q[i], z[t]);
+        }
+      }
+      if (more) load_keys(next_at);
+      const bool all = k0 >= lo_all.lo && k0 + 32 <= min(hi_all.hi, end) && there == 0xffffffffu;
+      // values to shared memory; rows that are not there as zeros, because a
+      // weight of zero does not take away a NaN
+#pragma unroll
+      for (int i = 0; i < F::vloads; ++i) {
+        const int key = i * F::vrows + lane / F::chunks, c = lane % F::chunks;
+        const bool is = there >> key & 1;
+        u32x4 x = vreg[i];
+        if (!is) x = u32x4{0, 0, 0, 0};
+        char *to = vbuf + key * F::row_bytes;
+        const int sw = few_swizzle<D>(key);
+        if constexpr (CODES) {
+          const u32x2 x0 = codes_to_half<TYPE>(x[0]), x1 = codes_to_half<TYPE>(x[1]);
+          const u32x2 x2 = codes_to_half<TYPE>(x[2]), x3 = codes_to_half<TYPE>(x[3]);
+          u32x4 y0 = {x0[0], x0[1], x1[0], x1[1]}, y1 = {x2[0], x2[1], x3[0], x3[1]};
+          if (TYPE == WS_KV_FP8 && !all) {
+            bad |= take_unbounded<BF>(y0);
+            bad |= take_unbounded<BF>(y1);
+          }
+          *reinterpret_cast<u32x4 *>(to + ((2 * c) ^ sw) * 16) = y0;
+          *reinterpret_cast<u32x4 *>(to + ((2 * c + 1) ^ sw) * 16) = y1;
+        } else {
+          if (!all) bad |= take_unbounded<BF>(x);
+          *reinterpret_cast<u32x4 *>(to + (c ^ sw) * 16) = x;
+        }
+      }
+      if (more) load_values(next_at);
+      row_at = next_at;
+      next_page = page_entry(a, b, k0 + 256 + mine, end);
+
+      float w[8], ref[8], vsc[8];
+      if constexpr (CODES) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const f32x4 sk = *reinterpret_cast<const f32x4 *>(kscale + 16 * t + 4 * g);
+          const f32x4 lv = *reinterpret_cast<const f32x4 *>(vlog + 16 * t + 4 * g);
+          const f32x4 sv = *reinterpret_cast<const f32x4 *>(vscale + 16 * t + 4 * g);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            w[4 * t + r] = z[t][r] * (by * sk[r]);
+            ref[4 * t + r] = lv[r];
+            vsc[4 * t + r] = sv[r];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = z[i / 4][i % 4] * by;
+      }
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int j = 16 * (i / 4) + 4 * g + i % 4;
+          const bool in = k0 + j >= see.lo && k0 + j < see.hi && (there >> j & 1);
+          if (!in) w[i] = -INFINITY;
+          if (CODES && !in) vsc[i] = 0.0f;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, CODES ? w[i] + ref[i] : w[i]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      top = fmaxf(top, m);
+      const float base = top == -INFINITY ? 0.0f : top;
+      const float shrink = exp2_of(m - base);
+      m = top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = exp2_of(w[i] - base);
+        sum += w[i];
+        if constexpr (CODES) w[i] *= vsc[i];
+      }
+      l = l * shrink + sum;
+      if (__any(shrink != 1.0f)) {
+#pragma unroll
+        for (int i = 0; i < F::tiles; ++i) o[i] *= shrink;
+      }
+      const u32x4 p = {pack2<BF>(w[0], w[1]), pack2<BF>(w[2], w[3]), pack2<BF>(w[4], w[5]),
+                       pack2<BF>(w[6], w[7])};
+      __builtin_amdgcn_wave_barrier();
+      const int key = 4 * g + n16 / 4;
+      const int sub = ((n16 & 3) >> 1) * 16 + (n16 & 1) * 8;
+      const char *v0 = vbuf + key * F::row_bytes + sub;
+      const char *v1 = v0 + 16 * F::row_bytes;
+      const int sw = few_swizzle<D>(key);  // the same for key + 16
+#pragma unroll
+      for (int i = 0; i < F::tiles; ++i) {
+        const int c = ((2 * i) ^ sw) * 16;
+        const u32x2 x = read_column(v0 + c), y = read_column(v1 + c);
+        o[i] = mfma16<BF>(u32x4{x[0], x[1], y[0], y[1]}, p, o[i]);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (__any(bad)) {
+      for (k0 = begin + 32 * wave; k0 < end; k0 += 128) {
+        const uint32_t there = (uint32_t)__ballot(
+            cache_row(a, page_entry(a, b, k0 + mine, end), h, k0 + mine, end) != kNoRow);
+        if (k0 >= lo_all.lo && k0 + 32 <= min(hi_all.hi, end) && there == 0xffffffffu) continue;
+        for (int32_t j = k0; j < min(k0 + 32, end); ++j) {
+          const int32_t at = cache_row(a, page_entry(a, b, j, end), h, j, end);
+          if (at == kNoRow || j < see.lo || j >= see.hi) continue;
+#pragma unroll
+          for (int i = 0; i < F::tiles; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              o[i][r] += unbounded_value<TYPE, D>(a, at, 16 * i + 4 * g + r);
+        }
+      }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // the four waves join through shared memory
+    __syncthreads();
+    float *jo = (float *)smem, *jm = jo + 4 * 16 * F::join_stride, *jl = jm + 64;
+#pragma unroll
+    for (int i = 0; i < F::tiles; ++i)
+      *reinterpret_cast<f32x4 *>(jo + (wave * 16 + n16) * F::join_stride + 16 * i + 4 * g) = o[i];
+    if (g == 0) {
+      jm[wave * 16 + n16] = m;
+      jl[wave * 16 + n16] = l;
+    }
+    __syncthreads();
+    constexpr int per = D / 4;  // threads of a row, four elements each
+    for (int r = threadIdx.x / per; r <= r1 - r0; r += 256 / per) {
+      const int d = threadIdx.x % per * 4;
+      float mw[4], top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, mw[i] = jm[i * 16 + r]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      float total = 0.0f;
+      f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = exp2_of(mw[i] - base);
+        total += jl[i * 16 + r] * e;
+        x += *reinterpret_cast<const f32x4 *>(jo + (i * 16 + r) * F::join_stride + d) * e;
+      }
+      const int32_t tok = (r0 + r) / a.group;
+      const int32_t hd = h * a.group + (r0 + r) - tok * a.group;
+      const int64_t q_row = s.q0 + tok;
+      if (parts == 1) {
+        const float inv = safe_inverse(total);
+        uint16_t *p = a.out + q_row * a.ot + (int64_t)hd * a.oh + d;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = out_bits(a, x[i] * inv);
+        if (a.lse && d == 0) a.lse[q_row * a.heads + hd] = natural_lse(top, total);
+      } else {
+        const int64_t to =
+            ((int64_t)(b * a.kv_heads + h) * kFewRows + r) * a.few_splits + split;
+        *reinterpret_cast<f32x4 *>(a.few_o + to * D + d) = x;
+        if (d == 0) a.few_ml[to] = make_float2(top, total);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------ many rows -------
+//
+// 128 rows of a request and KV head in a workgroup of four waves, 32 rows each;
+// tiles of keys and values in shared memory, two of each, so that the next is
+// written while this one is used.  Bound by the matrix instructions and, close
+// behind, the exponentials.
+
+constexpr int kManyRows = 128;
+
+template <int TYPE, int D>
+struct Many {
+  static constexpr int esz = kCodes<TYPE> ? 1 : 2;
+  static constexpr int keys = D == 256 ? 32 : 64;  // of a tile
+  static constexpr int ktiles = keys / 32;
+  static constexpr int steps = D / 16;             // of the product over d
+  static constexpr int tiles = D / 32;             // of the result
+  static constexpr int row_bytes = D * 2;
+  static constexpr int side = keys * row_bytes;    // a tile of keys, or of values
+  static constexpr int chunks = D * esz / 16;      // 16-byte loads of a row
+  static constexpr int rows = 256 / chunks;        // rows that 256 threads load at once
+  static constexpr int loads = keys / rows;
+  static constexpr int scales = kCodes<TYPE> ? keys * 12 : 0;
+  static constexpr int stage = 2 * side + scales + 16;  // one of the two buffers
+  static constexpr int smem = 2 * stage;
+};
+
+// Chunk c of key row `key`: keys are read 32 rows at one chunk, values 4 rows
+// of 64 bytes at a time.
+template <int D>
+__device__ __forceinline__ int key_swizzle(int key) {
+  return D == 64 ? (key >> 1) & 7 : key & 15;
+}
+template <int D>
+__device__ __forceinline__ int value_swizzle(int key) {
+  return D == 64 ? ((key >> 1) & 1) << 2 : (key & 3) << 2;
+}
+
+template <int TYPE, int D>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) many_rows_kernel(Args a) {
+  using M = Many<TYPE, D>;
+  constexpr bool BF = kBf<TYPE>;
+  constexpr bool CODES = kCodes<TYPE>;
+  __shared__ alignas(16) char smem[M::smem];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n32 = lane & 31, hh = lane >> 5;
+  // the row blocks of a request and head follow one another at a distance of
+  // n_seq * kv_heads workgroups: where that is a multiple of 8, they share one
+  // die's second level cache
+  const int32_t pairs = a.n_seq * a.kv_heads;
+  const int32_t at = blockIdx.x % pairs;
+  int32_t rest = blockIdx.x / pairs;
+  const int32_t h = at % a.kv_heads, b = at / a.kv_heads;
+  const int32_t split = rest % a.many_splits;
+  rest /= a.many_splits;
+  const Seq s = get_seq(a, b);
+  const int32_t rows = s.n * a.group;
+  if (rows <= kFewRows) return;
+  const int32_t blocks = (rows + kManyRows - 1) / kManyRows;
+
+  // the longest blocks, those of the last rows, first
+  for (int32_t nth = rest; nth < blocks; nth += a.row_blocks) {
+    const int32_t r0 = (blocks - 1 - nth) * kManyRows;
+    const int32_t r1 = min(r0 + kManyRows, rows) - 1;
+    const Range block = block_range(a, s, r0, r1, M::keys);
+    const int32_t parts = parts_of(block, a.many_chunk, a.many_splits);
+    if (split >= parts) continue;
+    const int32_t begin = block.lo + split * a.many_chunk;
+    const int32_t end = split == parts - 1 ? block.hi : begin + a.many_chunk;
+    const int32_t w0 = r0 + 32 * wave, w1 = min(w0 + 31, r1);  // this wave's rows
+    const int32_t row = w0 + n32;
+    const bool live = row <= r1;
+    const int32_t token = live ? row / a.group : r1 / a.group;
+    const int32_t head = h * a.group + (live ? row - token * a.group : 0);
+    Range see = token_range(a, s, token);
+    if (!live) see = {0, 0};
+    const bool any = w0 <= r1;
+    // keys that some row of the wave sees, and that all of them do
+    Range some = {0, 0}, every = {0, 0};
+    if (any) {
+      const Range first = token_range(a, s, w0 / a.group), last = token_range(a, s, w1 / a.group);
+      some = {first.lo, last.hi};
+      every = {last.lo, first.hi};
+    }
+
+    u32x4 q[M::steps];
+    float by = a.scale;
+    {
+      const uint16_t *p = a.q + (int64_t)(s.q0 + token) * a.qt + (int64_t)head * a.qh;
+      const bool wide = ((a.qt | a.qh) & 7) == 0 && ((uintptr_t)a.q & 15) == 0;
+#pragma unroll
+      for (int i = 0; i < M::steps; ++i) {
+        const int d = 16 * i + 8 * hh;
+        if (!live) {
+          q[i] = u32x4{0, 0, 0, 0};
+        } else if (wide) {
+          q[i] = *reinterpret_cast<const u32x4 *>(p + d);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            q[i][j] = (uint32_t)p[d + 2 * j] | (uint32_t)p[d + 2 * j + 1] << 16;
+        }
+      }
+      if (CODES && a.q_bf16) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < M::steps; ++i) top = max(top, top_of(q[i]));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const int e = row_exponent(top);
+#pragma unroll
+        for (int i = 0; i < M::steps; ++i) q[i] = bf16_to_half(q[i], ldexpf(1.0f, -e));
+        by *= ldexpf(1.0f, e);
+      }
+    }
+
+    f32x16 o[M::tiles];
+#pragma unroll
+    for (int i = 0; i < M::tiles; ++i) o[i] = f32x16{};
+    float m = -INFINITY, l = 0.0f;
+
+    const int lrow = threadIdx.x / M::chunks, lchunk = threadIdx.x % M::chunks;
+    u32x4 kreg[M::loads], vreg[M::loads];
+    int32_t page_at[M::loads], scale_page = 0;
+    uint32_t is = 0;        // loads whose rows are there
+    bool scale_is = false;  // whether key number lane is
+    float ks = 0.0f, vs = 0.0f;
+    auto find = [&](int32_t k0) {
+#pragma unroll
+      for (int i = 0; i < M::loads; ++i) page_at[i] = page_entry(a, b, k0 + i * M::rows + lrow, end);
+      scale_page = page_entry(a, b, k0 + (lane & (M::keys - 1)), end);
+    };
+    auto load = [&](int32_t k0) {
+      is = 0;
+#pragma unroll
+      for (int i = 0; i < M::loads; ++i) {
+        const int32_t at = cache_row(a, page_at[i], h, k0 + i * M::rows + lrow, end);
+        const int64_t r = (int64_t)max(at, 0) * (D * M::esz) + 16 * lchunk;
+        kreg[i] = *reinterpret_cast<const u32x4 *>(a.k + r);
+        vreg[i] = *reinterpret_cast<const u32x4 *>(a.v + r);
+        is |= (uint32_t)(at != kNoRow) << i;
+      }
+      const int32_t at = cache_row(a, scale_page, h, k0 + (lane & (M::keys - 1)), end);
+      scale_is = at != kNoRow;
+      if constexpr (CODES) {
+        if (wave == 0) {
+          ks = a.ks[max(at, 0)];
+          vs = a.vs[max(at, 0)];
+        }
+      }
+    };
+    // keys that every row of the block sees
+    const Range block_every = {token_range(a, s, r1 / a.group).lo, token_range(a, s, r0 / a.group).hi};
+    // keys and values that are not there go in as zeros
+    bool bad = false;  // a value was taken out
+    auto store = [&](char *to, int32_t k0) {
+      const bool edge = TYPE != WS_KV_INT8 && (k0 < block_every.lo || k0 + M::keys > block_every.hi);
+#pragma unroll
+      for (int i = 0; i < M::loads; ++i) {
+        const int key = i * M::rows + lrow;
+        char *kp = to + key * M::row_bytes, *vp = kp + M::side;
+        if (!(is >> i & 1)) {
+          kreg[i] = u32x4{0, 0, 0, 0};
+          vreg[i] = u32x4{0, 0, 0, 0};
+        }
+        const int ksw = key_swizzle<D>(key), vsw = value_swizzle<D>(key);
+        if constexpr (CODES) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const u32x2 x = codes_to_half<TYPE>(kreg[i][2 * c]), y = codes_to_half<TYPE>(kreg[i][2 * c + 1]);
+            *reinterpret_cast<u32x4 *>(kp + ((2 * lchunk + c) ^ ksw) * 16) = u32x4{x[0], x[1], y[0], y[1]};
+            const u32x2 u = codes_to_half<TYPE>(vreg[i][2 * c]), w = codes_to_half<TYPE>(vreg[i][2 * c + 1]);
+            u32x4 uw = {u[0], u[1], w[0], w[1]};
+            if (edge) bad |= take_unbounded<BF>(uw);
+            *reinterpret_cast<u32x4 *>(vp + ((2 * lchunk + c) ^ vsw) * 16) = uw;
+          }
+        } else {
+          *reinterpret_cast<u32x4 *>(kp + (lchunk ^ ksw) * 16) = kreg[i];
+          if (edge) bad |= take_unbounded<BF>(vreg[i]);
+          *reinterpret_cast<u32x4 *>(vp + (lchunk ^ vsw) * 16) = vreg[i];
+        }
+      }
+      float *sc = (float *)(to + 2 * M::side);
+      if (wave == 0) {
+        if (CODES && lane < M::keys) {
+          sc[lane] = ks;
+          sc[M::keys + lane] = fmaxf(log2f(vs), -110.0f);
+          sc[2 * M::keys + lane] = vs;
+        }
+        const uint64_t there = __ballot(lane < M::keys && scale_is);
+        if (lane == 0) *(uint64_t *)(to + 2 * M::side + M::scales) = there;
+      }
+    };
+
+    if (begin < end) {
+      find(begin);
+      load(begin);
+      find(begin + M::keys);
+      store(smem, begin);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int32_t k0 = begin; k0 < end; k0 += M::keys, buf ^= 1) {
+      const char *kb = smem + buf * M::stage, *vb = kb + M::side;
+      const bool more = k0 + M::keys < end;
+      if (more) {
+        load(k0 + M::keys);
+        find(k0 + 2 * M::keys);
+      }
+      if (any && k0 < some.hi && k0 + M::keys > some.lo) {
+        const uint64_t there = *(const uint64_t *)(kb + 2 * M::side + M::scales);
+        const uint32_t there_lo = (uint32_t)there, there_hi = (uint32_t)(there >> 32);
+        f32x16 z[M::ktiles];
+#pragma unroll
+        for (int t = 0; t < M::ktiles; ++t) {
+          z[t] = f32x16{};
+          const int key = 32 * t + n32;
+          const char *p = kb + key * M::row_bytes;
+          const int sw = key_swizzle<D>(key);
+#pragma unroll
+          for (int i = 0; i < M::steps; ++i) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(p + ((2 * i + hh) ^ sw) * 16);
+            z[t] = mfma32<BF>(x, q[i], z[t]);
+          }
+        }
+        // lane (n32, hh), register r of tile t: key 32 t + 8 (r / 4) + 4 hh + r % 4
+        const bool full = k0 >= every.lo && k0 + M::keys <= min(every.hi, end) &&
+                          (there_lo & (M::keys == 64 ? there_hi : 0xffffffffu)) == 0xffffffffu;
+        float top = -INFINITY;
+        const float *sc = (const float *)(kb + 2 * M::side);
+#pragma unroll
+        for (int t = 0; t < M::ktiles; ++t) {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            f32x4 sk, lv;
+            if constexpr (CODES) {
+              sk = *reinterpret_cast<const f32x4 *>(sc + 32 * t + 8 * r4 + 4 * hh);
+              lv = *reinterpret_cast<const f32x4 *>(sc + M::keys + 32 * t + 8 * r4 + 4 * hh);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float x = z[t][4 * r4 + r] * (CODES ? by * sk[r] : by);
+              if (!full) {
+                const int j = 8 * r4 + 4 * hh + r;
+                const int32_t key = k0 + 32 * t + j;
+                const bool in = key >= see.lo && key < see.hi && ((t ? there_hi : there_lo) >> j & 1);
+                if (!in) x = -INFINITY;
+              }
+              z[t][4 * r4 + r] = x;
+              top = fmaxf(top, CODES ? x + lv[r] : x);
+            }
+          }
+        }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        top = fmaxf(top, m);
+        const float base = top == -INFINITY ? 0.0f : top;
+        const float shrink = exp2_of(m - base);
+        m = top;
+        float sum = 0.0f;
+        u32x4 p[2 * M::ktiles];
+#pragma unroll
+        for (int t = 0; t < M::ktiles; ++t) {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            f32x4 w;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              w[r] = exp2_of(z[t][4 * r4 + r] - base);
+              sum += w[r];
+            }
+            if constexpr (CODES) {
+              const f32x4 sv = *reinterpret_cast<const f32x4 *>(sc + 2 * M::keys + 32 * t + 8 * r4 + 4 * hh);
+#pragma unroll
+              for (int r = 0; r < 4; ++r)  // a masked weight stays zero beside a scale of NaN
+                w[r] = !full && w[r] == 0.0f ? 0.0f : w[r] * sv[r];
+            }
+            p[2 * t + r4 / 2][2 * (r4 % 2)] = pack2<BF>(w[0], w[1]);
+            p[2 * t + r4 / 2][2 * (r4 % 2) + 1] = pack2<BF>(w[2], w[3]);
+          }
+        }
+        l = l * shrink + sum;
+        if (__any(shrink != 1.0f)) {
+#pragma unroll
+          for (int i = 0; i < M::tiles; ++i) o[i] *= shrink;
+        }
+        // p[c]: keys 16 c + 4 hh + (0..3) and + 8
+        const int i16 = lane & 15, q2 = (lane >> 4) & 1;
+        const int key = 4 * hh + i16 / 4;
+        const int vsw = value_swizzle<D>(key);  // the same for key + 8, + 16, ...
+        const char *v0 = vb + key * M::row_bytes + (i16 & 1) * 8;
+#pragma unroll
+        for (int i = 0; i < M::tiles; ++i) {
+          const int c = ((4 * i + 2 * q2 + ((i16 & 3) >> 1)) ^ vsw) * 16;
+#pragma unroll
+          for (int t = 0; t < 2 * M::ktiles; ++t) {
+            const u32x2 x = read_column(v0 + c + 16 * t * M::row_bytes);
+            const u32x2 y = read_column(v0 + c + (16 * t + 8) * M::row_bytes);
+            o[i] = mfma32<BF>(u32x4{x[0], x[1], y[0], y[1]}, p[t], o[i]);
+          }
+        }
+      }
+      if (more) store(smem + (buf ^ 1) * M::stage, k0 + M::keys);
+      __syncthreads();
+    }
+    if (TYPE != WS_KV_INT8 && __syncthreads_or(bad)) {
+      for (int32_t k0 = begin; k0 < end; k0 += M::keys) {
+        if (k0 >= block_every.lo && k0 + M::keys <= block_every.hi) continue;
+        for (int32_t j = k0; j < min(k0 + M::keys, end); ++j) {
+          const int32_t found = cache_row(a, page_entry(a, b, j, end), h, j, end);
+          if (found == kNoRow || j < see.lo || j >= see.hi) continue;
+#pragma unroll
+          for (int i = 0; i < M::tiles; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              o[i][r] += unbounded_value<TYPE, D>(a, found, 32 * i + 8 * (r / 4) + 4 * hh + r % 4);
+        }
+      }
+    }
+    l += __shfl_xor(l, 32);
+
+    // register r of o[i]: d = 32 i + 8 (r / 4) + 4 hh + r % 4 of row n32
+    if (live) {
+      const int64_t q_row = s.q0 + token;
+      if (parts == 1) {
+        const float inv = safe_inverse(l);
+        uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh;
+        const bool wide = ((a.ot | a.oh) & 3) == 0 && ((uintptr_t)a.out & 7) == 0;
+#pragma unroll
+        for (int i = 0; i < M::tiles; ++i) {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const int d = 32 * i + 8 * r4 + 4 * hh;
+            uint16_t x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = out_bits(a, o[i][4 * r4 + r] * inv);
+            if (wide) {
+              *reinterpret_cast<u32x2 *>(p + d) =
+                  u32x2{(uint32_t)x[0] | (uint32_t)x[1] << 16, (uint32_t)x[2] | (uint32_t)x[3] << 16};
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p[d + r] = x[r];
+            }
+          }
+        }
+        if (a.lse && hh == 0) a.lse[q_row * a.heads + head] = natural_lse(m, l);
+      } else {
+        const int64_t to = (q_row * a.heads + head) * a.many_splits + split;
+#pragma unroll
+        for (int i = 0; i < M::tiles; ++i)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4)
+            *reinterpret_cast<f32x4 *>(a.many_o + to * D + 32 * i + 8 * r4 + 4 * hh) =
+                f32x4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
+        if (hh == 0) a.many_ml[to] = make_float2(m, l);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ----------------------------------------------------------- joining ----
+//
+// A wave joins the parts of one (token, head): D / 64 elements a lane.
+
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(Args a, int32_t many_keys) {
+  constexpr int per = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int32_t head = id % a.heads, b = id / a.heads;
+  if (b >= a.n_seq) return;
+  const Seq s = get_seq(a, b);
+  const int32_t rows = s.n * a.group;
+  const bool few = !a.both || rows <= kFewRows;
+  for (int32_t i = blockIdx.y; i < s.n; i += gridDim.y) {
+    const int32_t row = i * a.group + head % a.group;
+    const int32_t unit = few ? kFewRows : kManyRows;
+    const int32_t r0 = row / unit * unit;
+    const Range block = block_range(a, s, r0, min(r0 + unit, rows) - 1, few ? 32 : many_keys);
+    const int32_t parts =
+        few ? few_parts(a, block, rows) : parts_of(block, a.many_chunk, a.many_splits);
+    if (parts == 1) continue;
+    const int64_t from =
+        few ? ((int64_t)(b * a.kv_heads + head / a.group) * kFewRows + row) * a.few_splits
+            : ((int64_t)(s.q0 + i) * a.heads + head) * a.many_splits;
+    const float2 *part_ml = few ? a.few_ml : a.many_ml;
+    const float *part_o = few ? a.few_o : a.many_o;
+    float top = -INFINITY;
+    for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, part_ml[from + k].x);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float base = top == -INFINITY ? 0.0f : top;
+    float total = 0.0f, o[per] = {};
+#pragma unroll 4
+    for (int32_t k = 0; k < parts; ++k) {
+      const float2 ml = part_ml[from + k];
+      const float e = exp2_of(ml.x - base);
+      total += ml.y * e;
+#pragma unroll
+      for (int j = 0; j < per; ++j) o[j] += part_o[(from + k) * D + lane * per + j] * e;
+    }
+    const float inv = safe_inverse(total);
+    const int64_t q_row = s.q0 + i;
+    uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + lane * per;
+#pragma unroll
+    for (int j = 0; j < per; ++j) p[j] = out_bits(a, o[j] * inv);
+    if (a.lse && lane == 0) a.lse[q_row * a.heads + head] = natural_lse(top, total);
+  }
+}
+
+// -------------------------------------------------------------- host -----
+
+// How a batch is laid out over workgroups.
+struct Layout {
+  bool many;
+  int32_t few_splits, few_chunk, many_splits, many_chunk, row_blocks;
+  int64_t few_slots, many_slots;  // results of parts in the workspace
+  int64_t bytes;
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Parts of at least `least` and at most `most` keys, multiples of `unit`, as
+// many as give `wanted` workgroups.
+void split_keys(int64_t keys, int64_t groups, int64_t wanted, int64_t least, int64_t most,
+                int32_t unit, int32_t *splits, int32_t *chunk) {
+  int64_t n = ceil_div(wanted, groups);
+  int64_t c = ceil_div(keys, n);
+  c = c < least ? least : c > most ? most : c;
+  c = ceil_div(c, unit) * unit;
+  *chunk = (int32_t)c;
+  *splits = (int32_t)(keys > c ? ceil_div(keys, c) : 1);
+}
+
+Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
+  Layout L{};
+  const int32_t group = b.heads / c.kv_heads;
+  int64_t max_q = b.max_q_len < 1 ? 1 : b.max_q_len;
+  int64_t max_kv = b.max_kv_len < 1 ? 1 : b.max_kv_len;
+  max_q = max_q > b.n_tokens ? b.n_tokens : max_q;
+  const int64_t capacity = (int64_t)b.table_cols * c.page_size;
+  max_kv = max_kv > capacity ? capacity : max_kv;
+  if (max_kv < 1) max_kv = 1;
+  const int64_t pairs = (int64_t)b.n_seq * c.kv_heads;
+  L.many = max_q * group > kFewRows;
+  int64_t few_keys = max_kv, many_keys = max_kv;
+  if (b.window) {
+    few_keys = std::min<int64_t>(max_kv, (int64_t)b.window + kFewRows + 32);
+    many_keys = std::min<int64_t>(max_kv, (int64_t)b.window + kManyRows + 64);
+  }
+  split_keys(few_keys, pairs, 1024, 256, 4096, 128, &L.few_splits, &L.few_chunk);
+  const int64_t blocks = ceil_div(max_q * group, kManyRows);
+  split_keys(many_keys, pairs * blocks, 512, 512, (int64_t)1 << 30, 64, &L.many_splits,
+             &L.many_chunk);
+  L.row_blocks = (int32_t)blocks;
+  if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_splits;
+  if (L.many && L.many_splits > 1)
+    L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
+  L.bytes = (L.few_slots + L.many_slots) * (c.dim + 2) * 4;
+  return L;
+}
+
+int check_batch(const ws_kv_cache *c, const ws_kv_batch *b) {
+  if (int rc = check_cache(c)) return rc;
+  if (!b) return invalid("attention: the batch must be non-NULL");
+  if (b->n_seq < 0 || b->n_tokens < 0 || b->heads < 1) return invalid("attention: bad sizes");
+  if (b->heads % c->kv_heads) return invalid("attention: heads must be a multiple of the cache's");
+  if (b->table_cols < 0 || b->table_stride < 0) return invalid("attention: bad page table");
+  if (!(b->scale > 0.0f) || !std::isfinite(b->scale))
+    return invalid("attention: the scale must be positive and finite");
+  if (b->window < 0) return invalid("attention: the window must not be negative");
+  if (b->max_q_len < 0 || b->max_kv_len < 0) return invalid("attention: bad length bounds");
+  if ((int64_t)b->n_tokens * b->heads >= (int64_t)1 << 31 ||
+      (int64_t)b->table_cols * c->page_size >= (int64_t)1 << 30)
+    return ws_record_failure(WS_EUNSUPPORTED,
+                             "attention: 2^31 rows or 2^30 keys a request, or more");
+  return WS_OK;
+}
+
+template <int TYPE, int D>
+int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
+  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
+  const int64_t few = pairs * L.few_splits, many = pairs * L.many_splits * L.row_blocks;
+  if (few >= (int64_t)1 << 31 || many >= (int64_t)1 << 31)
+    return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
+  if (L.many) {
+    many_rows_kernel<TYPE, D><<<dim3((uint32_t)many), 256, 0, stream>>>(a);
+    if (int rc = launched()) return rc;
+  }
+  few_rows_kernel<TYPE, D><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
+  if (int rc = launched()) return rc;
+  if (L.bytes) {
+    const uint32_t gx = (uint32_t)ceil_div((int64_t)a.n_seq * a.heads, 4);
+    const uint32_t gy = (uint32_t)std::min<int64_t>(L.row_blocks * (int64_t)kManyRows / a.group + 1, 1024);
+    join_kernel<D><<<dim3(gx, L.many ? gy : 1), 256, 0, stream>>>(a, Many<TYPE, D>::keys);
+    return launched();
+  }
+  return WS_OK;
+}
+
+template <int TYPE>
+int attention_dim(int dim, const Args &a, const Layout &L, hipStream_t stream) {
+  if (dim == 64) return attention_launch<TYPE, 64>(a, L, stream);
+  if (dim == 128) return attention_launch<TYPE, 128>(a, L, stream);
+  return attention_launch<TYPE, 256>(a, L, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int wait_kv_attention_workspace_bytes(const ws_kv_cache *cache, const ws_kv_batch *batch,
+                                      size_t *bytes) {
+  return guarded([&]() -> int {
+    if (!bytes) return invalid("bytes must be non-NULL");
+    if (int rc = check_batch(cache, batch)) return rc;
+    *bytes = batch->n_seq && batch->n_tokens ? (size_t)layout_of(*cache, *batch).bytes : 0;
+    return WS_OK;
+  });
+}
+
+int wait_kv_attention(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_kv_rows *q,
+                      const ws_kv_rows *out, float *lse, void *d_workspace, size_t ws_bytes,
+                      void *hip_stream) {
+  return guarded([&]() -> int {
+    if (int rc = check_batch(cache, batch)) return rc;
+    const ws_kv_batch &b = *batch;
+    if (int rc = check_rows(q, b.n_tokens, "attention: q must be non-NULL")) return rc;
+    if (int rc = check_rows(out, b.n_tokens, "attention: out must be non-NULL")) return rc;
+    if (q->type == WS_KV_FP32 || q->type != out->type)
+      return invalid("attention: q and out must both be bf16 or both fp16");
+    if (!is_8bit(cache->type) && q->type != cache->type)
+      return invalid("attention: q must have the type of a 16-bit cache");
+    if ((uintptr_t)lse % 4) return invalid("attention: lse must be aligned to 4 bytes");
+    if (b.n_seq == 0 || b.n_tokens == 0) return WS_OK;
+    if (!b.starts || !b.kv_lens || (b.table_cols > 0 && !b.table))
+      return invalid("attention: the page table, starts and lengths must be non-NULL");
+    if ((uintptr_t)b.starts % 4 || (uintptr_t)b.kv_lens % 4 || (uintptr_t)b.table % 4)
+      return invalid("attention: the page table, starts and lengths must be aligned to 4 bytes");
+    const Layout L = layout_of(*cache, b);
+    if (L.bytes && (!d_workspace || ws_bytes < (size_t)L.bytes))
+      return ws_record_failure(WS_EWORKSPACE, "attention: the workspace is too small");
+    if ((uintptr_t)d_workspace % 16) return invalid("attention: the workspace must be 16-byte aligned");
+    Args a{};
+    a.q = (const uint16_t *)q->data;
+    a.qt = q->token_stride;
+    a.qh = q->head_stride;
+    a.out = (uint16_t *)out->data;
+    a.ot = out->token_stride;
+    a.oh = out->head_stride;
+    a.lse = lse;
+    a.k = (const char *)cache->k;
+    a.v = (const char *)cache->v;
+    a.ks = cache->k_scale;
+    a.vs = cache->v_scale;
+    a.table = b.table;
+    a.table_stride = b.table_stride;
+    a.capacity = b.table_cols * cache->page_size;
+    a.starts = b.starts;
+    a.lens = b.kv_lens;
+    a.n_seq = b.n_seq;
+    a.n_tokens = b.n_tokens;
+    a.heads = b.heads;
+    a.kv_heads = cache->kv_heads;
+    a.group = b.heads / cache->kv_heads;
+    a.pages = cache->pages;
+    a.page_shift = log2_of(cache->page_size);
+    a.scale = (float)((double)b.scale * 1.4426950408889634074);
+    a.causal = b.causal != 0;
+    a.window = b.window;
+    a.q_bf16 = q->type == WS_KV_BF16;
+    if (L.bytes) {
+      a.few_o = (float *)d_workspace;
+      a.many_o = a.few_o + L.few_slots * cache->dim;
+      a.few_ml = (float2 *)(a.many_o + L.many_slots * cache->dim);
+      a.many_ml = a.few_ml + L.few_slots;
+    }
+    a.few_splits = L.few_splits;
+    a.few_chunk = L.few_chunk;
+    a.many_splits = L.many_splits;
+    a.many_chunk = L.many_chunk;
+    a.both = L.many;
+    a.row_blocks = L.row_blocks;
+    hipStream_t s = (hipStream_t)hip_stream;
+    switch (cache->type) {
+      case WS_KV_BF16: return attention_dim<WS_KV_BF16>(cache->dim, a, L, s);
+      case WS_KV_FP16: return attention_dim<WS_KV_FP16>(cache->dim, a, L, s);
+      case WS_KV_FP8: return attention_dim<WS_KV_FP8>(cache->dim, a, L, s);
+      default: return attention_dim<WS_KV_INT8>(cache->dim, a, L, s);
+    }
+  });
+}
+
+}  // extern "C"

@@ -1095,6 +1095,12 @@ uint8_t static_img[WS_STATIC_WORKSPACE_BYTES];
 
 }  // namespace
 
+// For the library's other translation units (kv_common.h).
+__attribute__((visibility("hidden"))) int ws_record_failure(int code, const char *msg) noexcept {
+  return fail(code, msg);
+}
+__attribute__((visibility("hidden"))) void ws_clear_failure() noexcept { g_err.clear(); }
+
 // ---------------------------------------------------------------- C ABI --
 
 extern "C" {
