@@ -47,9 +47,12 @@ struct Args {
   int32_t few_splits, few_chunk;    // of a few-rows launch: parts, keys a part
   int32_t many_splits, many_chunk;  // of a many-rows launch
   int32_t both;          // requests of more than 16 rows are the other launch's
-  int32_t row_blocks;
+  int32_t row_blocks;    // numbers of row blocks of the many-rows launch
 };
 
+#ifndef FEW_OCC
+#define FEW_OCC 2
+#endif
 constexpr int kFewRows = 16;
 
 // The queries of request b and its keys.
@@ -62,6 +65,20 @@ __device__ __forceinline__ Seq get_seq(const Args &a, int32_t b) {
   s.n = min(max(a.starts[b + 1], s.q0), a.n_tokens) - s.q0;
   s.m = max(a.lens[b], 0);
   return s;
+}
+
+// The last request for which `before` holds, which holds up to some request and
+// not behind it; -1 where for none.  A wave asks for 64 at once.
+template <class F>
+__device__ __forceinline__ int32_t last_at_most(const Args &a, F &&before) {
+  int32_t b = -1;
+  for (int32_t from = 0; from < a.n_seq; from += 64) {
+    const int32_t i = from + (threadIdx.x & 63);
+    const uint64_t yes = __ballot(i < a.n_seq && before(i));
+    b += __popcll(yes);
+    if (yes != ~0ull) break;
+  }
+  return __builtin_amdgcn_readfirstlane(b);
 }
 
 // Keys [lo, hi) that token i of the request sees.
@@ -251,7 +268,7 @@ __device__ __forceinline__ int few_swizzle(int key) {
 }
 
 template <int TYPE, int D>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a) {
+__global__ void __launch_bounds__(256, D == 256 ? 1 : FEW_OCC) few_rows_kernel(Args a) {
   using F = Few<TYPE, D>;
   constexpr bool BF = kBf<TYPE>;
   constexpr bool CODES = kCodes<TYPE>;
@@ -573,6 +590,11 @@ struct Many {
   static constexpr int smem = 2 * stage;
 };
 
+__device__ __forceinline__ int32_t first_block(const Args &a, int32_t b) {
+  const int32_t at = min(max(a.starts[b], 0), a.n_tokens);
+  return (int32_t)((int64_t)at * a.group / kManyRows) + b;
+}
+
 // Chunk c of key row `key`: keys are read 32 rows at one chunk, values 4 rows
 // of 64 bytes at a time.
 template <int D>
@@ -593,27 +615,28 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) many_rows_kernel(Args a
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
-  // the row blocks of a request and head follow one another at a distance of
-  // n_seq * kv_heads workgroups: where that is a multiple of 8, they share one
-  // die's second level cache
-  const int32_t pairs = a.n_seq * a.kv_heads;
-  const int32_t at = blockIdx.x % pairs;
-  int32_t rest = blockIdx.x / pairs;
-  const int32_t h = at % a.kv_heads, b = at / a.kv_heads;
-  const int32_t split = rest % a.many_splits;
-  rest /= a.many_splits;
+  // Workgroups are numbered (part, row block, head): where the KV heads are a
+  // multiple of 8, the row blocks of a head share one die's second level cache.
+  // The blocks of request b are those from floor(starts[b] * group / 128) + b on,
+  // which keeps requests apart and needs no count of the blocks before.
+  const int32_t h = blockIdx.x % a.kv_heads;
+  const int32_t rest = blockIdx.x / a.kv_heads;
+  const int32_t split = rest / a.row_blocks, nth = rest % a.row_blocks;
+  const int32_t b = last_at_most(a, [&](int32_t i) { return first_block(a, i) <= nth; });
+  if (b < 0) return;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
-  if (rows <= kFewRows) return;
   const int32_t blocks = (rows + kManyRows - 1) / kManyRows;
+  const int32_t back = nth - first_block(a, b);
+  if (rows <= kFewRows || back >= blocks) return;
 
-  // the longest blocks, those of the last rows, first
-  for (int32_t nth = rest; nth < blocks; nth += a.row_blocks) {
-    const int32_t r0 = (blocks - 1 - nth) * kManyRows;
+  {
+    // the longest blocks, those of the last rows, first
+    const int32_t r0 = (blocks - 1 - back) * kManyRows;
     const int32_t r1 = min(r0 + kManyRows, rows) - 1;
     const Range block = block_range(a, s, r0, r1, M::keys);
     const int32_t parts = parts_of(block, a.many_chunk, a.many_splits);
-    if (split >= parts) continue;
+    if (split >= parts) return;
     const int32_t begin = block.lo + split * a.many_chunk;
     const int32_t end = split == parts - 1 ? block.hi : begin + a.many_chunk;
     const int32_t w0 = r0 + 32 * wave, w1 = min(w0 + 31, r1);  // this wave's rows
@@ -902,58 +925,72 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) many_rows_kernel(Args a
         if (hh == 0) a.many_ml[to] = make_float2(m, l);
       }
     }
-    __syncthreads();
   }
 }
 
 // ----------------------------------------------------------- joining ----
 //
-// A wave joins the parts of one (token, head): D / 64 elements a lane.
+// A wave joins the parts of one (token, head), D / 64 elements a lane.
 
 template <int D>
-__global__ void __launch_bounds__(256) join_kernel(Args a, int32_t many_keys) {
+__device__ __forceinline__ void join_parts(const Args &a, const float *part_o, const float2 *part_ml,
+                                           int32_t parts, int64_t q_row, int32_t head) {
   constexpr int per = D / 64;
   const int lane = threadIdx.x & 63;
+  float top = -INFINITY;
+  for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, part_ml[k].x);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+  const float base = top == -INFINITY ? 0.0f : top;
+  float total = 0.0f, o[per] = {};
+#pragma unroll 8
+  for (int32_t k = 0; k < parts; ++k) {
+    const float2 ml = part_ml[k];
+    const float e = exp2_of(ml.x - base);
+    total += ml.y * e;
+#pragma unroll
+    for (int j = 0; j < per; ++j) o[j] += part_o[(int64_t)k * D + lane * per + j] * e;
+  }
+  const float inv = safe_inverse(total);
+  uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + lane * per;
+#pragma unroll
+  for (int j = 0; j < per; ++j) p[j] = out_bits(a, o[j] * inv);
+  if (a.lse && lane == 0) a.lse[q_row * a.heads + head] = natural_lse(top, total);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) join_few_kernel(Args a) {
   const int32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int32_t head = id % a.heads, b = id / a.heads;
   if (b >= a.n_seq) return;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
-  const bool few = !a.both || rows <= kFewRows;
-  for (int32_t i = blockIdx.y; i < s.n; i += gridDim.y) {
-    const int32_t row = i * a.group + head % a.group;
-    const int32_t unit = few ? kFewRows : kManyRows;
-    const int32_t r0 = row / unit * unit;
-    const Range block = block_range(a, s, r0, min(r0 + unit, rows) - 1, few ? 32 : many_keys);
-    const int32_t parts =
-        few ? few_parts(a, block, rows) : parts_of(block, a.many_chunk, a.many_splits);
-    if (parts == 1) continue;
-    const int64_t from =
-        few ? ((int64_t)(b * a.kv_heads + head / a.group) * kFewRows + row) * a.few_splits
-            : ((int64_t)(s.q0 + i) * a.heads + head) * a.many_splits;
-    const float2 *part_ml = few ? a.few_ml : a.many_ml;
-    const float *part_o = few ? a.few_o : a.many_o;
-    float top = -INFINITY;
-    for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, part_ml[from + k].x);
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float total = 0.0f, o[per] = {};
-#pragma unroll 4
-    for (int32_t k = 0; k < parts; ++k) {
-      const float2 ml = part_ml[from + k];
-      const float e = exp2_of(ml.x - base);
-      total += ml.y * e;
-#pragma unroll
-      for (int j = 0; j < per; ++j) o[j] += part_o[(from + k) * D + lane * per + j] * e;
-    }
-    const float inv = safe_inverse(total);
-    const int64_t q_row = s.q0 + i;
-    uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + lane * per;
-#pragma unroll
-    for (int j = 0; j < per; ++j) p[j] = out_bits(a, o[j] * inv);
-    if (a.lse && lane == 0) a.lse[q_row * a.heads + head] = natural_lse(top, total);
+  if (rows == 0 || rows > kFewRows) return;
+  const int32_t parts = few_parts(a, block_range(a, s, 0, rows - 1, 32), rows);
+  if (parts == 1) return;
+  const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * kFewRows;
+  for (int32_t i = 0; i < s.n; ++i) {
+    const int64_t at = (from + i * a.group + head % a.group) * a.few_splits;
+    join_parts<D>(a, a.few_o + at * D, a.few_ml + at, parts, s.q0 + i, head);
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) join_many_kernel(Args a, int32_t keys) {
+  const int32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int32_t head = id % a.heads, token = id / a.heads;
+  if (token >= a.n_tokens) return;
+  const int32_t b = last_at_most(a, [&](int32_t i) { return a.starts[i] <= token; });
+  if (b < 0) return;
+  const Seq s = get_seq(a, b);
+  const int32_t rows = s.n * a.group, i = token - s.q0;
+  if (i >= s.n || rows <= kFewRows) return;
+  const int32_t r0 = (i * a.group + head % a.group) / kManyRows * kManyRows;
+  const int32_t parts = parts_of(block_range(a, s, r0, min(r0 + kManyRows, rows) - 1, keys),
+                                 a.many_chunk, a.many_splits);
+  if (parts == 1) return;
+  const int64_t at = ((int64_t)token * a.heads + head) * a.many_splits;
+  join_parts<D>(a, a.many_o + at * D, a.many_ml + at, parts, token, head);
 }
 
 // -------------------------------------------------------------- host -----
@@ -997,10 +1034,10 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
     many_keys = std::min<int64_t>(max_kv, (int64_t)b.window + kManyRows + 64);
   }
   split_keys(few_keys, pairs, 1024, 256, 4096, 128, &L.few_splits, &L.few_chunk);
-  const int64_t blocks = ceil_div(max_q * group, kManyRows);
-  split_keys(many_keys, pairs * blocks, 512, 512, (int64_t)1 << 30, 64, &L.many_splits,
-             &L.many_chunk);
-  L.row_blocks = (int32_t)blocks;
+  L.row_blocks = (int32_t)((int64_t)b.n_tokens * group / kManyRows + b.n_seq);
+  // workgroups that have rows: as many as the tokens fill
+  const int64_t full = ceil_div((int64_t)b.n_tokens * group, kManyRows) * c.kv_heads;
+  split_keys(many_keys, full, 512, 256, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
   if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_splits;
   if (L.many && L.many_splits > 1)
     L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
@@ -1028,7 +1065,7 @@ int check_batch(const ws_kv_cache *c, const ws_kv_batch *b) {
 template <int TYPE, int D>
 int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
-  const int64_t few = pairs * L.few_splits, many = pairs * L.many_splits * L.row_blocks;
+  const int64_t few = pairs * L.few_splits, many = (int64_t)a.kv_heads * L.many_splits * L.row_blocks;
   if (few >= (int64_t)1 << 31 || many >= (int64_t)1 << 31)
     return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
   if (L.many) {
@@ -1037,13 +1074,14 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   }
   few_rows_kernel<TYPE, D><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
   if (int rc = launched()) return rc;
-  if (L.bytes) {
-    const uint32_t gx = (uint32_t)ceil_div((int64_t)a.n_seq * a.heads, 4);
-    const uint32_t gy = (uint32_t)std::min<int64_t>(L.row_blocks * (int64_t)kManyRows / a.group + 1, 1024);
-    join_kernel<D><<<dim3(gx, L.many ? gy : 1), 256, 0, stream>>>(a, Many<TYPE, D>::keys);
-    return launched();
+  if (L.few_slots) {
+    join_few_kernel<D><<<dim3((uint32_t)ceil_div((int64_t)a.n_seq * a.heads, 4)), 256, 0, stream>>>(a);
+    if (int rc = launched()) return rc;
   }
-  return WS_OK;
+  if (L.many_slots)
+    join_many_kernel<D><<<dim3((uint32_t)ceil_div((int64_t)a.n_tokens * a.heads, 4)), 256, 0,
+                          stream>>>(a, Many<TYPE, D>::keys);
+  return launched();
 }
 
 template <int TYPE>

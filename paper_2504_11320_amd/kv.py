@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from typing import Optional
 
 import torch
@@ -29,29 +30,12 @@ CACHE_TYPES = (torch.bfloat16, torch.float16, torch.float8_e4m3fn, torch.int8)
 EIGHT_BIT = (torch.float8_e4m3fn, torch.int8)
 
 
-class _Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
-                ("type", C.c_int32)]
-
-
-class _Turn(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("positions", C.c_void_p), ("positions_32", C.c_int32),
-                ("n_table", C.c_int32), ("part", C.c_int32), ("interleaved", C.c_int32)]
-
-
-class _Cache(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
-                ("v_scale", C.c_void_p), ("pages", C.c_int32), ("page_size", C.c_int32),
-                ("kv_heads", C.c_int32), ("dim", C.c_int32), ("type", C.c_int32)]
-
-
-class _Batch(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("table_cols", C.c_int32),
-                ("starts", C.c_void_p), ("kv_lens", C.c_void_p), ("n_seq", C.c_int32),
-                ("n_tokens", C.c_int32), ("heads", C.c_int32), ("scale", C.c_float),
-                ("causal", C.c_int32), ("window", C.c_int32), ("max_q_len", C.c_int32),
-                ("max_kv_len", C.c_int32)]
-
+# The structs of include/wait_kv.h, packed: a call's marshalling is most of a
+# small operator's time, and bytes cost a fraction of ctypes' structures.
+ROWS = struct.Struct("Pqqi4x")              # ws_kv_rows
+TURN = struct.Struct("PPiiii")              # ws_kv_turn
+CACHE = struct.Struct("PPPPiiiii4x")        # ws_kv_cache
+BATCH = struct.Struct("Pqi4xPPiiifiiii")    # ws_kv_batch
 
 _fn = None
 
@@ -60,20 +44,35 @@ def _lib():
     global _fn
     if _fn is None:
         L = B.lib()
-        rows, turn, cache, batch = (C.POINTER(t) for t in (_Rows, _Turn, _Cache, _Batch))
-        p, i64, i32 = C.c_void_p, C.c_int64, C.c_int32
-        L.wait_kv_rotary.argtypes = [rows, rows, i64, i32, i32, turn, i32, p]
-        L.wait_kv_append.argtypes = [cache, rows, rows, p, i64, turn, p]
-        L.wait_kv_read.argtypes = [cache, p, i64, rows, rows, p]
-        L.wait_kv_attention_workspace_bytes.argtypes = [cache, batch, C.POINTER(C.c_size_t)]
-        L.wait_kv_attention.argtypes = [cache, batch, rows, rows, p, p, C.c_size_t, p]
+        p, i64, i32, s = C.c_void_p, C.c_int64, C.c_int32, C.c_char_p
+        L.wait_kv_rotary.argtypes = [s, s, i64, i32, i32, s, i32, p]
+        L.wait_kv_append.argtypes = [s, s, s, p, i64, s, p]
+        L.wait_kv_read.argtypes = [s, p, i64, s, s, p]
+        L.wait_kv_attention_workspace_bytes.argtypes = [s, s, C.POINTER(C.c_size_t)]
+        L.wait_kv_attention.argtypes = [s, s, s, s, p, p, C.c_size_t, p]
         _fn = L
     return _fn
 
 
-def _stream(device) -> int:
-    _need(device.type == "cuda", "the operators run on the GPU")
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same without building a Stream object, where this PyTorch has it
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
+
+
+def _run(fn, index: int, *args):
+    """fn(*args, the current stream) on GPU number `index`."""
+    if index < 0:
+        raise ValueError("the operators run on the GPU")
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, _stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream(index))
+    if rc:
+        B._check(rc)
 
 
 def _need(ok: bool, msg: str):
@@ -81,16 +80,16 @@ def _need(ok: bool, msg: str):
         raise ValueError(msg)
 
 
-def _on(device, **tensors):
-    for name, t in tensors.items():
-        _need(t.device == device, f"{name} must be on {device}, is on {t.device}")
-
-
-def _rows(t: torch.Tensor, name: str, types=_WIDE) -> _Rows:
-    _need(t.dim() == 3, f"{name} must be [tokens, heads, dim]")
-    _need(t.dtype in types, f"{name} must be one of {types}, is {t.dtype}")
-    _need(t.stride(2) == 1 or t.shape[2] == 1, f"{name}: a vector's elements must be contiguous")
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1), _TYPE[t.dtype])
+def _rows(t: torch.Tensor, name: str, index: int, types=_WIDE) -> bytes:
+    """The struct of t [tokens, heads, dim], on GPU number `index`."""
+    step = t.stride()
+    dtype = t.dtype
+    if len(step) != 3 or dtype not in types or step[2] != 1 or t.get_device() != index:
+        _need(len(step) == 3, f"{name} must be [tokens, heads, dim]")
+        _need(dtype in types, f"{name} must be one of {types}, is {dtype}")
+        _need(step[2] == 1 or t.shape[2] == 1, f"{name}: a vector's elements must be contiguous")
+        _need(t.get_device() == index, f"{name} must be on the same device, is on {t.device}")
+    return ROWS.pack(t.data_ptr(), step[0], step[1], _TYPE[dtype])
 
 
 def _apart(t: torch.Tensor, name: str):
@@ -103,19 +102,26 @@ def _apart(t: torch.Tensor, name: str):
             need = abs(step) * (size - 1) + need
 
 
-def _turn(positions, table, n: int, dim: int, interleaved: bool, device) -> _Turn:
-    _need(positions is not None and table is not None, "a rotation needs positions and a table")
-    _need(table.dim() == 2 and table.dtype == torch.float32 and table.is_contiguous(),
-          "table must be [positions, part], fp32, contiguous")
-    _need(positions.dim() == 1 and positions.shape[0] == n and positions.is_contiguous()
-          and positions.dtype in (torch.int64, torch.int32),
-          "positions must be one int64 or int32 a token, contiguous")
-    part = table.shape[1]
-    _need(part % 2 == 0 and 2 <= part <= dim,
-          "the table's part must be even, at least 2 and at most the head dimension")
-    _on(device, positions=positions, table=table)
-    return _Turn(table.data_ptr(), positions.data_ptr(), positions.dtype == torch.int32,
-                 table.shape[0], part, bool(interleaved))
+def _turn(positions, table, n: int, dim: int, interleaved: bool, index: int) -> bytes:
+    if positions is None or table is None:
+        raise ValueError("a rotation needs positions and a table")
+    size = table.shape
+    kind = positions.dtype
+    if (len(size) != 2 or table.dtype is not torch.float32 or not table.is_contiguous()
+            or positions.shape != (n,) or not positions.is_contiguous()
+            or (kind is not torch.int64 and kind is not torch.int32) or size[1] % 2
+            or not 2 <= size[1] <= dim or positions.get_device() != index
+            or table.get_device() != index):
+        _need(len(size) == 2 and table.dtype == torch.float32 and table.is_contiguous(),
+              "table must be [positions, part], fp32, contiguous")
+        _need(positions.shape == (n,) and positions.is_contiguous()
+              and kind in (torch.int64, torch.int32),
+              "positions must be one int64 or int32 a token, contiguous")
+        _need(size[1] % 2 == 0 and 2 <= size[1] <= dim,
+              "the table's part must be even, at least 2 and at most the head dimension")
+        raise ValueError("positions and table must be on the vectors' device")
+    return TURN.pack(table.data_ptr(), positions.data_ptr(), kind is torch.int32, size[0], size[1],
+                     bool(interleaved))
 
 
 # ----------------------------------------------------------------- rotary ----
@@ -169,19 +175,18 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *,
     (2 i, 2 i + 1) where ``interleaved``.  ``inverse`` turns back; that is the
     gradient's way through a rotation.  ``out`` may be x.  A position outside
     the table gives NaN."""
-    L = _lib()
-    xr = _rows(x, "x")
+    fn = _lib().wait_kv_rotary
+    index = x.get_device()
+    xr = _rows(x, "x", index)
     n, heads, dim = x.shape
-    t = _turn(positions, table, n, dim, interleaved, x.device)
+    t = _turn(positions, table, n, dim, interleaved, index)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape and out.dtype == x.dtype, "out must have x's shape and type")
-    _on(x.device, out=out)
-    _apart(out, "out")
-    if n == 0 or heads == 0:
-        return out
-    B._check(L.wait_kv_rotary(xr, _rows(out, "out"), n, heads, dim, t, inverse,
-                              _stream(x.device)))
+        out = torch.empty_like(x)
+    else:
+        _need(out.shape == x.shape and out.dtype == x.dtype, "out must have x's shape and type")
+        _apart(out, "out")
+    if n and heads:
+        _run(fn, index, xr, _rows(out, "out", index), n, heads, dim, t, inverse)
     return out
 
 
@@ -197,26 +202,28 @@ class Cache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype,
+        size, dtype, index = k.shape, k.dtype, k.get_device()
+        _need(len(size) == 4 and size == v.shape and dtype is v.dtype,
               "k and v must both be [pages, kv_heads, page_size, dim] of one type")
-        _need(k.dtype in CACHE_TYPES, f"a cache's type is one of {CACHE_TYPES}")
+        _need(dtype in CACHE_TYPES, f"a cache's type is one of {CACHE_TYPES}")
         _need(k.is_contiguous() and v.is_contiguous(), "k and v must be contiguous")
-        _on(k.device, v=v)
-        ptr = [None, None]
-        if k.dtype in EIGHT_BIT:
+        _need(v.get_device() == index, "k and v must be on one device")
+        kp = vp = 0
+        if dtype in EIGHT_BIT:
             _need(k_scale is not None and v_scale is not None, "an 8-bit cache needs scales")
-            for i, (n, s) in enumerate((("k_scale", k_scale), ("v_scale", v_scale))):
-                _need(s.shape == k.shape[:3] and s.dtype == torch.float32 and s.is_contiguous(),
-                      f"{n} must be [pages, kv_heads, page_size], fp32, contiguous")
-                _on(k.device, **{n: s})
-                ptr[i] = s.data_ptr()
+            for t in (k_scale, v_scale):
+                _need(t.shape == size[:3] and t.dtype is torch.float32 and t.is_contiguous()
+                      and t.get_device() == index,
+                      "scales must be [pages, kv_heads, page_size], fp32, contiguous, on the "
+                      "cache's device")
+            kp, vp = k_scale.data_ptr(), v_scale.data_ptr()
         else:
             _need(k_scale is None and v_scale is None, "a 16-bit cache has no scales")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.pages, self.kv_heads, self.page_size, self.dim = k.shape
-        self.dtype, self.device = k.dtype, k.device
-        self._c = _Cache(k.data_ptr(), v.data_ptr(), ptr[0], ptr[1], self.pages, self.page_size,
-                         self.kv_heads, self.dim, _TYPE[k.dtype])
+        self.pages, self.kv_heads, self.page_size, self.dim = size
+        self.dtype, self.device, self._index = dtype, k.device, index
+        self._c = CACHE.pack(k.data_ptr(), v.data_ptr(), kp, vp, self.pages, self.page_size,
+                             self.kv_heads, self.dim, _TYPE[dtype])
 
     @classmethod
     def empty(cls, pages: int, page_size: int, kv_heads: int, dim: int,
@@ -233,11 +240,12 @@ class Cache:
         return 2 * kv_heads * (dim * dtype.itemsize + (4 if dtype in EIGHT_BIT else 0))
 
 
-def _slots(slots: torch.Tensor, device) -> int:
-    _need(slots.dim() == 1 and slots.dtype == torch.int64 and slots.is_contiguous(),
-          "slots must be one int64 a token, contiguous")
-    _on(device, slots=slots)
-    return slots.shape[0]
+def _slots(slots: torch.Tensor, index: int) -> int:
+    size = slots.shape
+    _need(len(size) == 1 and slots.dtype is torch.int64 and slots.is_contiguous()
+          and slots.get_device() == index,
+          "slots must be one int64 a token, contiguous, on the cache's device")
+    return size[0]
 
 
 def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *,
@@ -248,36 +256,37 @@ def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
     negative, or behind the cache's end, is left out.  With ``positions`` and
     ``table`` the keys are turned first, as by ``rotary``, without a rounding
     between."""
-    L = _lib()
-    kr, vr = _rows(k, "k"), _rows(v, "v")
-    n = _slots(slots, cache.device)
-    _need(k.shape == v.shape == (n, cache.kv_heads, cache.dim) and k.dtype == v.dtype,
+    fn = _lib().wait_kv_append
+    index = cache._index
+    kr, vr = _rows(k, "k", index), _rows(v, "v", index)
+    n = _slots(slots, index)
+    _need(k.shape == (n, cache.kv_heads, cache.dim) and k.shape == v.shape and k.dtype is v.dtype,
           "k and v must be [slots, kv_heads, dim] of one type")
-    _on(cache.device, k=k, v=v)
     t = None
     if positions is not None or table is not None:
-        t = _turn(positions, table, n, cache.dim, interleaved, cache.device)
-    B._check(L.wait_kv_append(cache._c, kr, vr, slots.data_ptr(), n, t, _stream(cache.device)))
+        t = _turn(positions, table, n, cache.dim, interleaved, index)
+    _run(fn, index, cache._c, kr, vr, slots.data_ptr(), n, t)
 
 
 def read(cache: Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
          out: Optional[tuple] = None) -> tuple:
     """(k, v) [slots, kv_heads, dim] of the cache's slots, as values rounded
     once to ``dtype``; zeros for a slot that the cache does not have."""
-    L = _lib()
-    n = _slots(slots, cache.device)
+    fn = _lib().wait_kv_read
+    index = cache._index
+    n = _slots(slots, index)
     shape = (n, cache.kv_heads, cache.dim)
     if out is None:
         _need(dtype in _WIDE, f"dtype must be one of {_WIDE}")
-        out = tuple(torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
-    k, v = out
-    _need(k.shape == v.shape == shape and k.dtype == v.dtype,
-          "out must be two [slots, kv_heads, dim] of one type")
-    _on(cache.device, k=k, v=v)
-    _apart(k, "k")
-    _apart(v, "v")
-    B._check(L.wait_kv_read(cache._c, slots.data_ptr(), n, _rows(k, "k"), _rows(v, "v"),
-                            _stream(cache.device)))
+        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        v = torch.empty_like(k)
+    else:
+        k, v = out
+        _need(k.shape == shape and v.shape == shape and k.dtype is v.dtype,
+              "out must be two [slots, kv_heads, dim] of one type")
+        _apart(k, "k")
+        _apart(v, "v")
+    _run(fn, index, cache._c, slots.data_ptr(), n, _rows(k, "k", index), _rows(v, "v", index))
     return k, v
 
 
@@ -305,50 +314,60 @@ def attention(q: torch.Tensor, cache: Cache, pages: torch.Tensor, starts: torch.
     tensor of ``attention_workspace_bytes``) is taken from PyTorch where it is
     not given."""
     L = _lib()
-    qr = _rows(q, "q", _WIDE[:2])
-    T, heads, dim = q.shape
-    _need(dim == cache.dim, "q and the cache must have one head dimension")
-    _need(heads >= 1 and heads % cache.kv_heads == 0, "heads must be a multiple of the cache's")
-    _need(cache.dtype in EIGHT_BIT or q.dtype == cache.dtype,
+    index = cache._index
+    qr = _rows(q, "q", index, _WIDE[:2])
+    size = q.shape
+    _need(size[2] == cache.dim, "q and the cache must have one head dimension")
+    _need(cache.dtype in EIGHT_BIT or q.dtype is cache.dtype,
           "q must have the type of a 16-bit cache")
-    batch = _batch(q, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, causal, window)
+    batch, need = _batch(size, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, causal,
+                         window)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape and out.dtype == q.dtype, "out must have q's shape and type")
-    _on(cache.device, q=q, out=out)
-    _apart(out, "out")
-    lse = torch.empty((T, heads), device=q.device) if return_lse else None
-    need = C.c_size_t()
-    B._check(L.wait_kv_attention_workspace_bytes(cache._c, batch, need))
-    if need.value and workspace is None:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-    ptr, size = None, 0
+        out = torch.empty_like(q)
+    else:
+        _need(out.shape == size and out.dtype is q.dtype, "out must have q's shape and type")
+        _apart(out, "out")
+    lse = torch.empty(size[:2], dtype=torch.float32, device=q.device) if return_lse else None
+    ptr, have = None, 0
     if workspace is not None:
-        _need(workspace.is_contiguous(), "workspace must be contiguous")
-        _on(cache.device, workspace=workspace)
-        ptr, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    B._check(L.wait_kv_attention(cache._c, batch, qr, _rows(out, "out"),
-                                 lse.data_ptr() if return_lse else None, ptr, size,
-                                 _stream(q.device)))
-    return (out, lse) if return_lse else out
+        _need(workspace.is_contiguous() and workspace.get_device() == index,
+              "workspace must be contiguous, on the cache's device")
+        ptr, have = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ptr, have = workspace.data_ptr(), need
+    _run(L.wait_kv_attention, index, cache._c, batch, qr, _rows(out, "out", index),
+         None if lse is None else lse.data_ptr(), ptr, have)
+    return out if lse is None else (out, lse)
 
 
-def _batch(q, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, causal, window):
-    _need(pages.dim() == 2 and pages.dtype == torch.int32
-          and (pages.stride(1) == 1 or pages.shape[1] <= 1),
-          "pages must be [requests, pages], int32, rows contiguous")
-    n_seq = pages.shape[0]
-    for name, t, size in (("starts", starts, n_seq + 1), ("kv_lens", kv_lens, n_seq)):
-        _need(t.dim() == 1 and t.shape[0] == size and t.dtype == torch.int32
-              and t.is_contiguous(), f"{name} must be {size} int32, contiguous")
-    _on(cache.device, pages=pages, starts=starts, kv_lens=kv_lens)
-    T, heads, dim = q.shape
-    cap = pages.shape[1] * cache.page_size
-    return _Batch(pages.data_ptr(), pages.stride(0) if n_seq > 1 else pages.shape[1],
-                  pages.shape[1], starts.data_ptr(), kv_lens.data_ptr(), n_seq, T, heads,
-                  1.0 / math.sqrt(dim) if scale is None else scale, bool(causal), window,
-                  T if max_q_len is None else min(max_q_len, T),
-                  cap if max_kv_len is None else min(max_kv_len, cap))
+def _batch(size, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, causal, window):
+    """(the struct of a batch, the bytes of its workspace)."""
+    index = cache._index
+    T, heads, dim = size
+    n_seq, cols = pages.shape if pages.dim() == 2 else (-1, 0)
+    step = pages.stride()
+    if (n_seq < 0 or pages.dtype is not torch.int32 or (step[1] != 1 and cols > 1)
+            or pages.get_device() != index):
+        raise ValueError("pages must be [requests, pages], int32, rows contiguous, on the cache's "
+                         "device")
+    for t, n in ((starts, n_seq + 1), (kv_lens, n_seq)):
+        if (t.shape != (n,) or t.dtype is not torch.int32 or not t.is_contiguous()
+                or t.get_device() != index):
+            raise ValueError("starts (one more than the requests) and kv_lens (one each) must be "
+                             "int32, contiguous, on the cache's device")
+    _need(heads >= 1 and heads % cache.kv_heads == 0, "heads must be a multiple of the cache's")
+    cap = cols * cache.page_size
+    b = BATCH.pack(pages.data_ptr(), step[0] if n_seq > 1 else cols, cols, starts.data_ptr(),
+                   kv_lens.data_ptr(), n_seq, T, heads,
+                   1.0 / math.sqrt(dim) if scale is None else scale, bool(causal), window,
+                   T if max_q_len is None else min(max_q_len, T),
+                   cap if max_kv_len is None else min(max_kv_len, cap))
+    need = C.c_size_t()
+    rc = _lib().wait_kv_attention_workspace_bytes(cache._c, b, need)
+    if rc:
+        B._check(rc)
+    return b, need.value
 
 
 def attention_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor,
@@ -356,7 +375,5 @@ def attention_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor
                               max_q_len: Optional[int] = None, max_kv_len: Optional[int] = None,
                               window: int = 0) -> int:
     """Bytes that ``attention`` takes as its workspace for these shapes."""
-    b = _batch(q, cache, pages, starts, kv_lens, max_q_len, max_kv_len, None, True, window)
-    need = C.c_size_t()
-    B._check(_lib().wait_kv_attention_workspace_bytes(cache._c, b, need))
-    return need.value
+    return _batch(q.shape, cache, pages, starts, kv_lens, max_q_len, max_kv_len, None, True,
+                  window)[1]

@@ -28,24 +28,28 @@ def cache(**kw):
     d = dict(k=FAKE, v=FAKE, k_scale=None, v_scale=None, pages=4, page_size=16, kv_heads=2, dim=64,
              type=kv.BF16)
     d.update(kw)
-    return kv._Cache(*[d[n] for n, _ in kv._Cache._fields_])
+    return kv.CACHE.pack(*[d[n] or 0 for n in ("k", "v", "k_scale", "v_scale", "pages", "page_size",
+                                               "kv_heads", "dim", "type")])
 
 
 def rows(data=FAKE, token=128, head=64, type=kv.BF16):
-    return kv._Rows(data, token, head, type)
+    return kv.ROWS.pack(data or 0, token, head, type)
 
 
 def turn(**kw):
     d = dict(table=FAKE, positions=FAKE, positions_32=0, n_table=10, part=32, interleaved=0)
     d.update(kw)
-    return kv._Turn(*[d[n] for n, _ in kv._Turn._fields_])
+    return kv.TURN.pack(*[d[n] or 0 for n in ("table", "positions", "positions_32", "n_table",
+                                              "part", "interleaved")])
 
 
 def batch(**kw):
     d = dict(table=FAKE, table_stride=8, table_cols=8, starts=FAKE, kv_lens=FAKE, n_seq=2,
              n_tokens=4, heads=4, scale=1.0, causal=1, window=0, max_q_len=2, max_kv_len=100)
     d.update(kw)
-    return kv._Batch(*[d[n] for n, _ in kv._Batch._fields_])
+    return kv.BATCH.pack(*[d[n] or 0 for n in ("table", "table_stride", "table_cols", "starts",
+                                               "kv_lens", "n_seq", "n_tokens", "heads", "scale",
+                                               "causal", "window", "max_q_len", "max_kv_len")])
 
 
 def test_rotary_refusals():
