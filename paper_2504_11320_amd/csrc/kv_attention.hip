@@ -50,9 +50,6 @@ struct Args {
   int32_t row_blocks;    // numbers of row blocks of the many-rows launch
 };
 
-#ifndef FEW_OCC
-#define FEW_OCC 2
-#endif
 constexpr int kFewRows = 16;
 
 // The queries of request b and its keys.
@@ -123,8 +120,9 @@ __device__ __forceinline__ int32_t page_entry(const Args &a, int32_t b, int32_t 
 }
 __device__ __forceinline__ int32_t cache_row(const Args &a, int32_t page, int32_t h, int32_t j,
                                              int32_t end) {
-  if (j >= end || (uint32_t)page >= (uint32_t)a.pages) return kNoRow;
-  return ((page * a.kv_heads + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+  const bool is = (j < end) & ((uint32_t)page < (uint32_t)a.pages);
+  const int32_t row = ((page * a.kv_heads + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+  return is ? row : kNoRow;
 }
 
 template <bool BF>
@@ -217,7 +215,10 @@ __device__ __forceinline__ float unbounded_value(const Args &a, int32_t row, int
   else if constexpr (TYPE == WS_KV_FP16)
     x = Fp16::get(((const uint16_t *)a.v)[(int64_t)row * D + d]);
   else
-    x = (((const uint8_t *)a.v)[(int64_t)row * D + d] & 0x7f) == 0x7f ? NAN : 0.0f;
+    x = !isfinite(a.vs[row]) ||
+                (TYPE == WS_KV_FP8 && (((const uint8_t *)a.v)[(int64_t)row * D + d] & 0x7f) == 0x7f)
+            ? NAN
+            : 0.0f;
   return isfinite(x) ? 0.0f : x;
 }
 
@@ -268,7 +269,7 @@ __device__ __forceinline__ int few_swizzle(int key) {
 }
 
 template <int TYPE, int D>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : FEW_OCC) few_rows_kernel(Args a) {
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a) {
   using F = Few<TYPE, D>;
   constexpr bool BF = kBf<TYPE>;
   constexpr bool CODES = kCodes<TYPE>;
@@ -376,7 +377,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : FEW_OCC) few_rows_kernel(A
       const bool more = k0 + 128 < end;
       const int32_t next_at = cache_row(a, next_page, h, k0 + 128 + mine, end);
       const uint32_t there = (uint32_t)__ballot(row_at != kNoRow);
+      const bool all = k0 >= lo_all.lo && k0 + 32 <= min(hi_all.hi, end) && there == 0xffffffffu;
       if constexpr (CODES) {
+        if (!all && !isfinite(vs)) {
+          bad |= row_at != kNoRow;
+          vs = 0.0f;
+        }
         if (lane < 32) {
           kscale[lane] = ks;
           // below 2^-110 the reference no longer follows, the weight still does
@@ -405,7 +411,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : FEW_OCC) few_rows_kernel(A
         }
       }
       if (more) load_keys(next_at);
-      const bool all = k0 >= lo_all.lo && k0 + 32 <= min(hi_all.hi, end) && there == 0xffffffffu;
       // values to shared memory; rows that are not there as zeros, because a
       // weight of zero does not take away a NaN
 #pragma unroll
@@ -459,7 +464,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : FEW_OCC) few_rows_kernel(A
           const int j = 16 * (i / 4) + 4 * g + i % 4;
           const bool in = k0 + j >= see.lo && k0 + j < see.hi && (there >> j & 1);
           if (!in) w[i] = -INFINITY;
-          if (CODES && !in) vsc[i] = 0.0f;
         }
       }
       float top = -INFINITY;
@@ -566,16 +570,27 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : FEW_OCC) few_rows_kernel(A
 
 // ------------------------------------------------------ many rows -------
 //
-// 128 rows of a request and KV head in a workgroup of four waves, 32 rows each;
-// tiles of keys and values in shared memory, two of each, so that the next is
-// written while this one is used.  Bound by the matrix instructions and, close
-// behind, the exponentials.
+// 256 rows of a request and KV head in a workgroup of eight waves, 32 rows each;
+// tiles of keys and of values in shared memory, two of each.  Two waves share a
+// SIMD, and they take turns: while the one multiplies, the other does its
+// softmax, with a barrier at each change, so that the matrix and the vector
+// units both have work.  (D = 256: four waves of 32 rows, for want of
+// registers.)  Bound by the matrix instructions and, close behind, the
+// exponentials.
 
-constexpr int kManyRows = 128;
+// for the scheduler: kinds of instructions, and products whose operands are read
+// ahead
+constexpr int kMatrix = 0x8, kLdsRead = 0x100;
+constexpr int kAhead = 6;
+
+template <int D>
+constexpr int kManyRows = D == 256 ? 128 : 256;
 
 template <int TYPE, int D>
 struct Many {
   static constexpr int esz = kCodes<TYPE> ? 1 : 2;
+  static constexpr int groups = D == 256 ? 1 : 2;  // that take turns
+  static constexpr int threads = 256 * groups;
   static constexpr int keys = D == 256 ? 32 : 64;  // of a tile
   static constexpr int ktiles = keys / 32;
   static constexpr int steps = D / 16;             // of the product over d
@@ -583,20 +598,39 @@ struct Many {
   static constexpr int row_bytes = D * 2;
   static constexpr int side = keys * row_bytes;    // a tile of keys, or of values
   static constexpr int chunks = D * esz / 16;      // 16-byte loads of a row
-  static constexpr int rows = 256 / chunks;        // rows that 256 threads load at once
-  static constexpr int loads = keys / rows;
+  static constexpr int loads = 2 * keys * chunks / threads;  // of a thread, keys and values
   static constexpr int scales = kCodes<TYPE> ? keys * 12 : 0;
-  static constexpr int stage = 2 * side + scales + 16;  // one of the two buffers
-  static constexpr int smem = 2 * stage;
+  static constexpr int smem = 4 * side + 2 * scales;
 };
 
-__device__ __forceinline__ int32_t first_block(const Args &a, int32_t b) {
-  const int32_t at = min(max(a.starts[b], 0), a.n_tokens);
-  return (int32_t)((int64_t)at * a.group / kManyRows) + b;
+// 16 bytes a lane from memory to shared memory, the lanes' one after another
+// from `to` on, without a register between.  They are there after
+// await_copies(), for this wave; the compiler knows of neither.
+__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to))
+               : "memory");
+}
+__device__ __forceinline__ void await_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A loaded value is waited for here.  Left to its first use inside a loop, the
+// wait would be for every load that is outstanding there.
+template <class T>
+__device__ __forceinline__ void here_by_now(T &x) {
+  asm volatile("" : "+v"(x));
 }
 
-// Chunk c of key row `key`: keys are read 32 rows at one chunk, values 4 rows
-// of 64 bytes at a time.
+// The first row block of request b: blocks are numbered so that they need no
+// count of those before, and no two requests share one.
+template <int D>
+__device__ __forceinline__ int32_t first_block(const Args &a, int32_t b) {
+  const int32_t at = min(max(a.starts[b], 0), a.n_tokens);
+  return (int32_t)((int64_t)at * a.group / kManyRows<D>) + b;
+}
+
+// Chunk c of key row `key` lies at chunk c ^ swizzle: keys are read 32 rows at
+// one chunk, values 4 rows of 64 bytes at a time.
 template <int D>
 __device__ __forceinline__ int key_swizzle(int key) {
   return D == 64 ? (key >> 1) & 7 : key & 15;
@@ -607,7 +641,7 @@ __device__ __forceinline__ int value_swizzle(int key) {
 }
 
 template <int TYPE, int D>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) many_rows_kernel(Args a) {
+__global__ void __launch_bounds__(D == 256 ? 256 : 512, D == 256 ? 1 : 2) many_rows_kernel(Args a) {
   using M = Many<TYPE, D>;
   constexpr bool BF = kBf<TYPE>;
   constexpr bool CODES = kCodes<TYPE>;
@@ -615,316 +649,425 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) many_rows_kernel(Args a
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
-  // Workgroups are numbered (part, row block, head): where the KV heads are a
-  // multiple of 8, the row blocks of a head share one die's second level cache.
-  // The blocks of request b are those from floor(starts[b] * group / 128) + b on,
-  // which keeps requests apart and needs no count of the blocks before.
+  // the blocks of a head that run together read the same keys
   const int32_t h = blockIdx.x % a.kv_heads;
-  const int32_t rest = blockIdx.x / a.kv_heads;
-  const int32_t split = rest / a.row_blocks, nth = rest % a.row_blocks;
-  const int32_t b = last_at_most(a, [&](int32_t i) { return first_block(a, i) <= nth; });
+  const int32_t work = blockIdx.x / a.kv_heads;
+  const int32_t split = work / a.row_blocks, nth = work % a.row_blocks;
+  const int32_t b = last_at_most(a, [&](int32_t i) { return first_block<D>(a, i) <= nth; });
   if (b < 0) return;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
-  const int32_t blocks = (rows + kManyRows - 1) / kManyRows;
-  const int32_t back = nth - first_block(a, b);
+  const int32_t blocks = (rows + kManyRows<D> - 1) / kManyRows<D>;
+  const int32_t back = nth - first_block<D>(a, b);
   if (rows <= kFewRows || back >= blocks) return;
+  // the longest blocks, those of the last rows, first
+  const int32_t r0 = (blocks - 1 - back) * kManyRows<D>;
+  const int32_t r1 = min(r0 + kManyRows<D>, rows) - 1;
+  const Range block = block_range(a, s, r0, r1, M::keys);
+  const int32_t parts = parts_of(block, a.many_chunk, a.many_splits);
+  if (split >= parts) return;
+  const int32_t begin = block.lo + split * a.many_chunk;
+  const int32_t end = split == parts - 1 ? block.hi : begin + a.many_chunk;
+  const int32_t n = (end - begin + M::keys - 1) / M::keys;  // tiles
+  const int32_t w0 = r0 + 32 * wave, w1 = min(w0 + 31, r1);  // this wave's rows
+  const int32_t row = w0 + n32;
+  const bool live = row <= r1;
+  const int32_t token = live ? row / a.group : r1 / a.group;
+  const int32_t head = h * a.group + (live ? row - token * a.group : 0);
+  Range see = token_range(a, s, token);
+  if (!live) see = {0, 0};
+  // keys that some row of the wave sees, that all of them do, and all of the
+  // block
+  Range some = {0, 0}, every = {0, 0};
+  if (w0 <= r1) {
+    const Range first = token_range(a, s, w0 / a.group), last = token_range(a, s, w1 / a.group);
+    some = {first.lo, last.hi};
+    every = {last.lo, first.hi};
+  }
+  const Range block_every = {token_range(a, s, r1 / a.group).lo, token_range(a, s, r0 / a.group).hi};
 
+  u32x4 q[M::steps];
+  float by = a.scale;
   {
-    // the longest blocks, those of the last rows, first
-    const int32_t r0 = (blocks - 1 - back) * kManyRows;
-    const int32_t r1 = min(r0 + kManyRows, rows) - 1;
-    const Range block = block_range(a, s, r0, r1, M::keys);
-    const int32_t parts = parts_of(block, a.many_chunk, a.many_splits);
-    if (split >= parts) return;
-    const int32_t begin = block.lo + split * a.many_chunk;
-    const int32_t end = split == parts - 1 ? block.hi : begin + a.many_chunk;
-    const int32_t w0 = r0 + 32 * wave, w1 = min(w0 + 31, r1);  // this wave's rows
-    const int32_t row = w0 + n32;
-    const bool live = row <= r1;
-    const int32_t token = live ? row / a.group : r1 / a.group;
-    const int32_t head = h * a.group + (live ? row - token * a.group : 0);
-    Range see = token_range(a, s, token);
-    if (!live) see = {0, 0};
-    const bool any = w0 <= r1;
-    // keys that some row of the wave sees, and that all of them do
-    Range some = {0, 0}, every = {0, 0};
-    if (any) {
-      const Range first = token_range(a, s, w0 / a.group), last = token_range(a, s, w1 / a.group);
-      some = {first.lo, last.hi};
-      every = {last.lo, first.hi};
-    }
-
-    u32x4 q[M::steps];
-    float by = a.scale;
-    {
-      const uint16_t *p = a.q + (int64_t)(s.q0 + token) * a.qt + (int64_t)head * a.qh;
-      const bool wide = ((a.qt | a.qh) & 7) == 0 && ((uintptr_t)a.q & 15) == 0;
+    const uint16_t *p = a.q + (int64_t)(s.q0 + token) * a.qt + (int64_t)head * a.qh;
+    const bool wide = ((a.qt | a.qh) & 7) == 0 && ((uintptr_t)a.q & 15) == 0;
 #pragma unroll
-      for (int i = 0; i < M::steps; ++i) {
-        const int d = 16 * i + 8 * hh;
-        if (!live) {
-          q[i] = u32x4{0, 0, 0, 0};
-        } else if (wide) {
-          q[i] = *reinterpret_cast<const u32x4 *>(p + d);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            q[i][j] = (uint32_t)p[d + 2 * j] | (uint32_t)p[d + 2 * j + 1] << 16;
-        }
-      }
-      if (CODES && a.q_bf16) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < M::steps; ++i) top = max(top, top_of(q[i]));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const int e = row_exponent(top);
-#pragma unroll
-        for (int i = 0; i < M::steps; ++i) q[i] = bf16_to_half(q[i], ldexpf(1.0f, -e));
-        by *= ldexpf(1.0f, e);
-      }
-    }
-
-    f32x16 o[M::tiles];
-#pragma unroll
-    for (int i = 0; i < M::tiles; ++i) o[i] = f32x16{};
-    float m = -INFINITY, l = 0.0f;
-
-    const int lrow = threadIdx.x / M::chunks, lchunk = threadIdx.x % M::chunks;
-    u32x4 kreg[M::loads], vreg[M::loads];
-    int32_t page_at[M::loads], scale_page = 0;
-    uint32_t is = 0;        // loads whose rows are there
-    bool scale_is = false;  // whether key number lane is
-    float ks = 0.0f, vs = 0.0f;
-    auto find = [&](int32_t k0) {
-#pragma unroll
-      for (int i = 0; i < M::loads; ++i) page_at[i] = page_entry(a, b, k0 + i * M::rows + lrow, end);
-      scale_page = page_entry(a, b, k0 + (lane & (M::keys - 1)), end);
-    };
-    auto load = [&](int32_t k0) {
-      is = 0;
-#pragma unroll
-      for (int i = 0; i < M::loads; ++i) {
-        const int32_t at = cache_row(a, page_at[i], h, k0 + i * M::rows + lrow, end);
-        const int64_t r = (int64_t)max(at, 0) * (D * M::esz) + 16 * lchunk;
-        kreg[i] = *reinterpret_cast<const u32x4 *>(a.k + r);
-        vreg[i] = *reinterpret_cast<const u32x4 *>(a.v + r);
-        is |= (uint32_t)(at != kNoRow) << i;
-      }
-      const int32_t at = cache_row(a, scale_page, h, k0 + (lane & (M::keys - 1)), end);
-      scale_is = at != kNoRow;
-      if constexpr (CODES) {
-        if (wave == 0) {
-          ks = a.ks[max(at, 0)];
-          vs = a.vs[max(at, 0)];
-        }
-      }
-    };
-    // keys that every row of the block sees
-    const Range block_every = {token_range(a, s, r1 / a.group).lo, token_range(a, s, r0 / a.group).hi};
-    // keys and values that are not there go in as zeros
-    bool bad = false;  // a value was taken out
-    auto store = [&](char *to, int32_t k0) {
-      const bool edge = TYPE != WS_KV_INT8 && (k0 < block_every.lo || k0 + M::keys > block_every.hi);
-#pragma unroll
-      for (int i = 0; i < M::loads; ++i) {
-        const int key = i * M::rows + lrow;
-        char *kp = to + key * M::row_bytes, *vp = kp + M::side;
-        if (!(is >> i & 1)) {
-          kreg[i] = u32x4{0, 0, 0, 0};
-          vreg[i] = u32x4{0, 0, 0, 0};
-        }
-        const int ksw = key_swizzle<D>(key), vsw = value_swizzle<D>(key);
-        if constexpr (CODES) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const u32x2 x = codes_to_half<TYPE>(kreg[i][2 * c]), y = codes_to_half<TYPE>(kreg[i][2 * c + 1]);
-            *reinterpret_cast<u32x4 *>(kp + ((2 * lchunk + c) ^ ksw) * 16) = u32x4{x[0], x[1], y[0], y[1]};
-            const u32x2 u = codes_to_half<TYPE>(vreg[i][2 * c]), w = codes_to_half<TYPE>(vreg[i][2 * c + 1]);
-            u32x4 uw = {u[0], u[1], w[0], w[1]};
-            if (edge) bad |= take_unbounded<BF>(uw);
-            *reinterpret_cast<u32x4 *>(vp + ((2 * lchunk + c) ^ vsw) * 16) = uw;
-          }
-        } else {
-          *reinterpret_cast<u32x4 *>(kp + (lchunk ^ ksw) * 16) = kreg[i];
-          if (edge) bad |= take_unbounded<BF>(vreg[i]);
-          *reinterpret_cast<u32x4 *>(vp + (lchunk ^ vsw) * 16) = vreg[i];
-        }
-      }
-      float *sc = (float *)(to + 2 * M::side);
-      if (wave == 0) {
-        if (CODES && lane < M::keys) {
-          sc[lane] = ks;
-          sc[M::keys + lane] = fmaxf(log2f(vs), -110.0f);
-          sc[2 * M::keys + lane] = vs;
-        }
-        const uint64_t there = __ballot(lane < M::keys && scale_is);
-        if (lane == 0) *(uint64_t *)(to + 2 * M::side + M::scales) = there;
-      }
-    };
-
-    if (begin < end) {
-      find(begin);
-      load(begin);
-      find(begin + M::keys);
-      store(smem, begin);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int32_t k0 = begin; k0 < end; k0 += M::keys, buf ^= 1) {
-      const char *kb = smem + buf * M::stage, *vb = kb + M::side;
-      const bool more = k0 + M::keys < end;
-      if (more) {
-        load(k0 + M::keys);
-        find(k0 + 2 * M::keys);
-      }
-      if (any && k0 < some.hi && k0 + M::keys > some.lo) {
-        const uint64_t there = *(const uint64_t *)(kb + 2 * M::side + M::scales);
-        const uint32_t there_lo = (uint32_t)there, there_hi = (uint32_t)(there >> 32);
-        f32x16 z[M::ktiles];
-#pragma unroll
-        for (int t = 0; t < M::ktiles; ++t) {
-          z[t] = f32x16{};
-          const int key = 32 * t + n32;
-          const char *p = kb + key * M::row_bytes;
-          const int sw = key_swizzle<D>(key);
-#pragma unroll
-          for (int i = 0; i < M::steps; ++i) {
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(p + ((2 * i + hh) ^ sw) * 16);
-            z[t] = mfma32<BF>(x, q[i], z[t]);
-          }
-        }
-        // lane (n32, hh), register r of tile t: key 32 t + 8 (r / 4) + 4 hh + r % 4
-        const bool full = k0 >= every.lo && k0 + M::keys <= min(every.hi, end) &&
-                          (there_lo & (M::keys == 64 ? there_hi : 0xffffffffu)) == 0xffffffffu;
-        float top = -INFINITY;
-        const float *sc = (const float *)(kb + 2 * M::side);
-#pragma unroll
-        for (int t = 0; t < M::ktiles; ++t) {
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            f32x4 sk, lv;
-            if constexpr (CODES) {
-              sk = *reinterpret_cast<const f32x4 *>(sc + 32 * t + 8 * r4 + 4 * hh);
-              lv = *reinterpret_cast<const f32x4 *>(sc + M::keys + 32 * t + 8 * r4 + 4 * hh);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float x = z[t][4 * r4 + r] * (CODES ? by * sk[r] : by);
-              if (!full) {
-                const int j = 8 * r4 + 4 * hh + r;
-                const int32_t key = k0 + 32 * t + j;
-                const bool in = key >= see.lo && key < see.hi && ((t ? there_hi : there_lo) >> j & 1);
-                if (!in) x = -INFINITY;
-              }
-              z[t][4 * r4 + r] = x;
-              top = fmaxf(top, CODES ? x + lv[r] : x);
-            }
-          }
-        }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        top = fmaxf(top, m);
-        const float base = top == -INFINITY ? 0.0f : top;
-        const float shrink = exp2_of(m - base);
-        m = top;
-        float sum = 0.0f;
-        u32x4 p[2 * M::ktiles];
-#pragma unroll
-        for (int t = 0; t < M::ktiles; ++t) {
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            f32x4 w;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              w[r] = exp2_of(z[t][4 * r4 + r] - base);
-              sum += w[r];
-            }
-            if constexpr (CODES) {
-              const f32x4 sv = *reinterpret_cast<const f32x4 *>(sc + 2 * M::keys + 32 * t + 8 * r4 + 4 * hh);
-#pragma unroll
-              for (int r = 0; r < 4; ++r)  // a masked weight stays zero beside a scale of NaN
-                w[r] = !full && w[r] == 0.0f ? 0.0f : w[r] * sv[r];
-            }
-            p[2 * t + r4 / 2][2 * (r4 % 2)] = pack2<BF>(w[0], w[1]);
-            p[2 * t + r4 / 2][2 * (r4 % 2) + 1] = pack2<BF>(w[2], w[3]);
-          }
-        }
-        l = l * shrink + sum;
-        if (__any(shrink != 1.0f)) {
-#pragma unroll
-          for (int i = 0; i < M::tiles; ++i) o[i] *= shrink;
-        }
-        // p[c]: keys 16 c + 4 hh + (0..3) and + 8
-        const int i16 = lane & 15, q2 = (lane >> 4) & 1;
-        const int key = 4 * hh + i16 / 4;
-        const int vsw = value_swizzle<D>(key);  // the same for key + 8, + 16, ...
-        const char *v0 = vb + key * M::row_bytes + (i16 & 1) * 8;
-#pragma unroll
-        for (int i = 0; i < M::tiles; ++i) {
-          const int c = ((4 * i + 2 * q2 + ((i16 & 3) >> 1)) ^ vsw) * 16;
-#pragma unroll
-          for (int t = 0; t < 2 * M::ktiles; ++t) {
-            const u32x2 x = read_column(v0 + c + 16 * t * M::row_bytes);
-            const u32x2 y = read_column(v0 + c + (16 * t + 8) * M::row_bytes);
-            o[i] = mfma32<BF>(u32x4{x[0], x[1], y[0], y[1]}, p[t], o[i]);
-          }
-        }
-      }
-      if (more) store(smem + (buf ^ 1) * M::stage, k0 + M::keys);
-      __syncthreads();
-    }
-    if (TYPE != WS_KV_INT8 && __syncthreads_or(bad)) {
-      for (int32_t k0 = begin; k0 < end; k0 += M::keys) {
-        if (k0 >= block_every.lo && k0 + M::keys <= block_every.hi) continue;
-        for (int32_t j = k0; j < min(k0 + M::keys, end); ++j) {
-          const int32_t found = cache_row(a, page_entry(a, b, j, end), h, j, end);
-          if (found == kNoRow || j < see.lo || j >= see.hi) continue;
-#pragma unroll
-          for (int i = 0; i < M::tiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              o[i][r] += unbounded_value<TYPE, D>(a, found, 32 * i + 8 * (r / 4) + 4 * hh + r % 4);
-        }
-      }
-    }
-    l += __shfl_xor(l, 32);
-
-    // register r of o[i]: d = 32 i + 8 (r / 4) + 4 hh + r % 4 of row n32
-    if (live) {
-      const int64_t q_row = s.q0 + token;
-      if (parts == 1) {
-        const float inv = safe_inverse(l);
-        uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh;
-        const bool wide = ((a.ot | a.oh) & 3) == 0 && ((uintptr_t)a.out & 7) == 0;
-#pragma unroll
-        for (int i = 0; i < M::tiles; ++i) {
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            const int d = 32 * i + 8 * r4 + 4 * hh;
-            uint16_t x[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = out_bits(a, o[i][4 * r4 + r] * inv);
-            if (wide) {
-              *reinterpret_cast<u32x2 *>(p + d) =
-                  u32x2{(uint32_t)x[0] | (uint32_t)x[1] << 16, (uint32_t)x[2] | (uint32_t)x[3] << 16};
-            } else {
-#pragma unroll
-              for (int r = 0; r < 4; ++r) p[d + r] = x[r];
-            }
-          }
-        }
-        if (a.lse && hh == 0) a.lse[q_row * a.heads + head] = natural_lse(m, l);
+    for (int i = 0; i < M::steps; ++i) {
+      const int d = 16 * i + 8 * hh;
+      if (!live) {
+        q[i] = u32x4{0, 0, 0, 0};
+      } else if (wide) {
+        q[i] = *reinterpret_cast<const u32x4 *>(p + d);
       } else {
-        const int64_t to = (q_row * a.heads + head) * a.many_splits + split;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          q[i][j] = (uint32_t)p[d + 2 * j] | (uint32_t)p[d + 2 * j + 1] << 16;
+      }
+    }
+    if (CODES && a.q_bf16) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < M::steps; ++i) top = max(top, top_of(q[i]));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+      const int e = row_exponent(top);
+#pragma unroll
+      for (int i = 0; i < M::steps; ++i) q[i] = bf16_to_half(q[i], ldexpf(1.0f, -e));
+      by *= ldexpf(1.0f, e);
+    }
+#pragma unroll
+    for (int i = 0; i < M::steps; ++i) here_by_now(q[i]);
+  }
+
+  f32x16 o[M::tiles];
+#pragma unroll
+  for (int i = 0; i < M::tiles; ++i) o[i] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+
+  // Tiles on their way.  In step t the keys of tile t + 1 and the values of tile
+  // t come in.  Each lane finds the row of one key of a tile; 16-bit tiles go
+  // from memory to shared memory directly, codes through registers, where they
+  // become halves.
+  const uint32_t shared = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  const int32_t mine = lane & (M::keys - 1);
+  int32_t page = 0, key_row = 0;
+  uint64_t key_there = 0, value_there = 0, there_before = 0;  // rows that are there
+  u32x4 reg[CODES ? M::loads : 1];
+  float ks = 0.0f, vs = 0.0f;
+  bool bad = false;  // a value was taken out
+  auto is_value = [&](int i) {  // whether load i is one of values
+    return M::loads > 1 ? i >= M::loads / 2 : wave >= 4;
+  };
+  auto key_of = [&](int i) {
+    return (i * M::threads + (int)threadIdx.x) / M::chunks % M::keys;
+  };
+  int32_t at[M::loads];  // rows of this thread's loads
+  auto spread = [&](int32_t keys, int32_t values) {
+#pragma unroll
+    for (int i = 0; i < M::loads; ++i)
+      at[i] = __builtin_amdgcn_ds_bpermute(4 * key_of(i), is_value(i) ? values : keys);
+  };
+  auto find = [&](int32_t t, uint64_t &there) {  // this lane's key's row, of tile t
+    const int32_t found = cache_row(a, page, h, begin + t * M::keys + mine, end);
+    there = __ballot(found != kNoRow);
+    return max(found, 0);
+  };
+  auto ask = [&](int32_t t) { page = page_entry(a, b, begin + t * M::keys + mine, end); };
+  // The end of step t: the rows of step t + 1, and the pages of that behind it.
+  // (In step t + 1 itself, waiting for them would be waiting for its copies.)
+  auto look = [&](int32_t t) {
+    there_before = value_there;
+    value_there = key_there;
+    const int32_t values = key_row;
+    key_row = find(t + 2, key_there);
+    spread(key_row, values);
+    ask(t + 3);
+  };
+  auto load = [&](int32_t t, bool keys, bool values) {
+#pragma unroll
+    for (int i = 0; i < M::loads; ++i) {
+      if (!(is_value(i) ? values : keys)) continue;
+      const char *from = (is_value(i) ? a.v : a.k) + (uint64_t)(uint32_t)at[i] * (D * M::esz);
+      const int c = threadIdx.x % M::chunks;
+      if constexpr (CODES) {
+        reg[i] = *reinterpret_cast<const u32x4 *>(from + 16 * c);
+      } else {
+        // shared memory is filled in order, so the swizzle is in what is read
+        const int sw = is_value(i) ? value_swizzle<D>(key_of(i)) : key_swizzle<D>(key_of(i));
+        const int tile = is_value(i) ? 2 + (t & 1) : (t + 1) & 1;
+        const int first = (i % (M::loads / 2) * M::threads + wave * 64) * 16;
+        copy_to_lds(from + 16 * (c ^ sw), shared + tile * M::side + first);
+      }
+    }
+    if (CODES && keys && wave == 0) {
+      ks = a.ks[key_row];
+      vs = a.vs[key_row];
+    }
+  };
+  // What load(t) asked for is there, and in its place: rows that are not there
+  // as zeros, because a weight of zero does not take away a NaN.
+  auto arrive = [&](int32_t t, bool keys, bool values) {
+    const int32_t k0 = begin + t * M::keys, k1 = k0 + M::keys;
+    const bool edge = k0 < block_every.lo || k1 > block_every.hi;
+    if constexpr (CODES) {
+#pragma unroll
+      for (int i = 0; i < M::loads; ++i) {
+        const bool v = is_value(i);
+        if (!(v ? values : keys)) continue;
+        const int key = key_of(i), c = threadIdx.x % M::chunks;
+        const int tile = v ? 2 + (t & 1) : (t + 1) & 1;
+        const int sw = v ? value_swizzle<D>(key) : key_swizzle<D>(key);
+        char *to = smem + tile * M::side + key * M::row_bytes;
+        u32x4 x = reg[i];
+        if (!((v ? value_there : key_there) >> key & 1)) x = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const u32x2 y = codes_to_half<TYPE>(x[2 * half]), z = codes_to_half<TYPE>(x[2 * half + 1]);
+          u32x4 w = {y[0], y[1], z[0], z[1]};
+          if (TYPE == WS_KV_FP8 && v && edge) bad |= take_unbounded<BF>(w);
+          *reinterpret_cast<u32x4 *>(to + ((2 * c + half) ^ sw) * 16) = w;
+        }
+      }
+      if (keys && wave == 0 && lane < M::keys) {
+        const bool next_edge = k1 < block_every.lo || k1 + M::keys > block_every.hi;
+        if (next_edge && !isfinite(vs)) {
+          bad |= key_there >> lane & 1;
+          vs = 0.0f;
+        }
+        float *sc = (float *)(smem + 4 * M::side + ((t + 1) & 1) * M::scales);
+        sc[lane] = ks;
+        // below 2^-110 the reference no longer follows, the weight still does
+        sc[M::keys + lane] = fmaxf(log2f(vs), -110.0f);
+        sc[2 * M::keys + lane] = vs;
+      }
+    } else {
+      await_copies();
+      if (values && (edge || value_there != ~0ull)) {
+#pragma unroll
+        for (int i = 0; i < M::loads / 2; ++i) {
+          u32x4 *at = (u32x4 *)(smem + (2 + (t & 1)) * M::side + (i * M::threads + threadIdx.x) * 16);
+          u32x4 x = *at;
+          if (!(value_there >> key_of(i) & 1)) x = u32x4{0, 0, 0, 0};
+          if (edge) bad |= take_unbounded<BF>(x);
+          *at = x;
+        }
+      }
+    }
+  };
+  // Scores of tile t: lane (n32, hh), register r of z[k]: key 32 k + 8 (r / 4) +
+  // 4 hh + r % 4.  Their weights p[c]: keys 16 c + 4 hh + (0..3) and + 8.
+  f32x16 z[M::ktiles];
+  u32x4 p[2 * M::ktiles];
+  auto add_values = [&](int32_t t) {
+    const char *vb = smem + (2 + (t & 1)) * M::side;
+    const int i16 = lane & 15, q2 = (lane >> 4) & 1;
+    const int key = 4 * hh + i16 / 4;
+    const int sw = value_swizzle<D>(key);  // the same for key + 8, + 16, ...
+    const char *v0 = vb + key * M::row_bytes + (i16 & 1) * 8;
+#pragma unroll
+    for (int c = 0; c < 2 * M::ktiles; ++c) {
+#pragma unroll
+      for (int i = 0; i < M::tiles; ++i) {
+        const char *at = v0 + ((4 * i + 2 * q2 + ((i16 & 3) >> 1)) ^ sw) * 16 + 16 * c * M::row_bytes;
+        const u32x2 x = read_column(at), y = read_column(at + 8 * M::row_bytes);
+        o[i] = mfma32<BF>(u32x4{x[0], x[1], y[0], y[1]}, p[c], o[i]);
+      }
+    }
+  };
+  auto score = [&](int32_t t) {
+    const char *kb = smem + (t & 1) * M::side + n32 * M::row_bytes;
+    const int sw = key_swizzle<D>(n32);  // the same for key + 32
+#pragma unroll
+    for (int k = 0; k < M::ktiles; ++k) z[k] = f32x16{};
+#pragma unroll
+    for (int i = 0; i < M::steps; ++i) {
+#pragma unroll
+      for (int k = 0; k < M::ktiles; ++k) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(kb + 32 * k * M::row_bytes +
+                                                         ((2 * i + hh) ^ sw) * 16);
+        z[k] = mfma32<BF>(x, q[i], z[k]);
+      }
+    }
+  };
+  // Products run 32 cycles each, a read from shared memory takes a few times
+  // that: kAhead products' reads are under way before the first.
+  auto multiply = [&](int32_t t) {
+    __builtin_amdgcn_s_setprio(1);
+    add_values(t - 1);
+    score(t);
+    constexpr int pv = 2 * M::ktiles * M::tiles, qk = M::ktiles * M::steps;
+    __builtin_amdgcn_sched_group_barrier(kLdsRead, 2 * kAhead, 0);
+#pragma unroll
+    for (int i = 0; i < pv - kAhead; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < qk; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead, 0);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  auto weigh = [&](int32_t t, uint64_t there) {
+    const int32_t k0 = begin + t * M::keys;
+    if (k0 >= some.hi || k0 + M::keys <= some.lo) {  // none that this wave sees
+#pragma unroll
+      for (int c = 0; c < 2 * M::ktiles; ++c) p[c] = u32x4{0, 0, 0, 0};
+      return;
+    }
+    const uint32_t there_lo = (uint32_t)there, there_hi = (uint32_t)(there >> 32);
+    const bool full = k0 >= every.lo && k0 + M::keys <= min(every.hi, end) && there == ~0ull;
+    const float *sc = (const float *)(smem + 4 * M::side + (t & 1) * M::scales);
+    auto scales = [&](int which, int k, int r4) {
+      return *reinterpret_cast<const f32x4 *>(sc + which * M::keys + 32 * k + 8 * r4 + 4 * hh);
+    };
+    if constexpr (CODES) {
+#pragma unroll
+      for (int k = 0; k < M::ktiles; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 sk = scales(0, k, r / 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[k][r + e] *= sk[e];
+        }
+    }
+    if (!full) {
+#pragma unroll
+      for (int k = 0; k < M::ktiles; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = 8 * (r / 4) + 4 * hh + r % 4;
+          const int32_t key = k0 + 32 * k + j;
+          const bool in = (key >= see.lo) & (key < see.hi) & ((k ? there_hi : there_lo) >> j & 1);
+          z[k][r] = in ? z[k][r] : -INFINITY;
+        }
+    }
+    // the largest score, times log2(e) and the scale; of codes, plus log2 of the
+    // value's scale
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < M::ktiles; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        f32x4 x = {z[k][r], z[k][r + 1], z[k][r + 2], z[k][r + 3]};
+        if constexpr (CODES) {
+          const f32x4 lv = scales(1, k, r / 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(x[e], by, lv[e]);
+        }
+        top = fmaxf(fmaxf(top, x[0]), x[1]);
+        top = fmaxf(fmaxf(top, x[2]), x[3]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(CODES ? top : top * by, m);
+    const float base = top == -INFINITY ? 0.0f : top;
+    const float shrink = exp2_of(m - base);
+    m = top;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < 2 * M::ktiles; ++c) {
+#pragma unroll
+      for (int r4 = 0; r4 < 2; ++r4) {
+        f32x4 w;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          w[r] = exp2_of(__builtin_fmaf(z[c / 2][8 * (c % 2) + 4 * r4 + r], by, -base));
+          sum[r4] += w[r];
+        }
+        if constexpr (CODES) w *= scales(2, c / 2, 2 * (c % 2) + r4);
+        p[c][2 * r4] = pack2<BF>(w[0], w[1]);
+        p[c][2 * r4 + 1] = pack2<BF>(w[2], w[3]);
+      }
+    }
+    l = l * shrink + (sum[0] + sum[1]);
+    if (__any(shrink != 1.0f)) {
+#pragma unroll
+      for (int i = 0; i < M::tiles; ++i) o[i] *= shrink;
+    }
+  };
+
+  if (n > 0) {
+    ask(0);
+    const int32_t first = find(0, key_there);
+    key_row = first;
+    ask(1);
+    spread(first, first);
+    load(-1, true, false);
+    arrive(-1, true, false);
+    value_there = key_there;
+    key_row = find(1, key_there);
+    spread(key_row, first);
+    ask(2);
+    __syncthreads();
+    // step t: the first waves multiply for tile t and weigh it, the others weigh
+    // tile t - 1 and multiply for t
+    load(0, n > 1, true);
+    if (M::groups == 1 || wave < 4) {
+      score(0);
+      __syncthreads();
+      weigh(0, value_there);
+      arrive(0, n > 1, true);
+      look(0);
+      __syncthreads();
+      for (int32_t t = 1; t < n; ++t) {
+        load(t, t + 1 < n, true);
+        multiply(t);
+        __syncthreads();
+        weigh(t, value_there);
+        arrive(t, t + 1 < n, true);
+        look(t);
+        __syncthreads();
+      }
+    } else {
+      __syncthreads();
+      score(0);
+      arrive(0, n > 1, true);
+      look(0);
+      __syncthreads();
+      for (int32_t t = 1; t < n; ++t) {
+        load(t, t + 1 < n, true);
+        weigh(t - 1, there_before);
+        __syncthreads();
+        multiply(t);
+        arrive(t, t + 1 < n, true);
+        look(t);
+        __syncthreads();
+      }
+      weigh(n - 1, there_before);
+    }
+    add_values(n - 1);
+  }
+  if (__syncthreads_or(bad)) {
+    for (int32_t k0 = begin; k0 < end; k0 += M::keys) {
+      if (k0 >= block_every.lo && k0 + M::keys <= block_every.hi) continue;
+      for (int32_t j = k0; j < min(k0 + M::keys, end); ++j) {
+        const int32_t found = cache_row(a, page_entry(a, b, j, end), h, j, end);
+        if (found == kNoRow || j < see.lo || j >= see.hi) continue;
 #pragma unroll
         for (int i = 0; i < M::tiles; ++i)
 #pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4)
-            *reinterpret_cast<f32x4 *>(a.many_o + to * D + 32 * i + 8 * r4 + 4 * hh) =
-                f32x4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
-        if (hh == 0) a.many_ml[to] = make_float2(m, l);
+          for (int r = 0; r < 16; ++r)
+            o[i][r] += unbounded_value<TYPE, D>(a, found, 32 * i + 8 * (r / 4) + 4 * hh + r % 4);
       }
     }
+  }
+  l += __shfl_xor(l, 32);
+
+  // register r of o[i]: d = 32 i + 8 (r / 4) + 4 hh + r % 4 of row n32
+  if (!live) return;
+  const int64_t q_row = s.q0 + token;
+  if (parts == 1) {
+    const float inv = safe_inverse(l);
+    uint16_t *to = a.out + q_row * a.ot + (int64_t)head * a.oh;
+    const bool wide = ((a.ot | a.oh) & 3) == 0 && ((uintptr_t)a.out & 7) == 0;
+#pragma unroll
+    for (int i = 0; i < M::tiles; ++i) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int d = 32 * i + 8 * r4 + 4 * hh;
+        uint16_t x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = out_bits(a, o[i][4 * r4 + r] * inv);
+        if (wide) {
+          *reinterpret_cast<u32x2 *>(to + d) =
+              u32x2{(uint32_t)x[0] | (uint32_t)x[1] << 16, (uint32_t)x[2] | (uint32_t)x[3] << 16};
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) to[d + r] = x[r];
+        }
+      }
+    }
+    if (a.lse && hh == 0) a.lse[q_row * a.heads + head] = natural_lse(m, l);
+  } else {
+    const int64_t to = (q_row * a.heads + head) * a.many_splits + split;
+#pragma unroll
+    for (int i = 0; i < M::tiles; ++i)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4 *>(a.many_o + to * D + 32 * i + 8 * r4 + 4 * hh) =
+            f32x4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
+    if (hh == 0) a.many_ml[to] = make_float2(m, l);
   }
 }
 
@@ -985,8 +1128,8 @@ __global__ void __launch_bounds__(256) join_many_kernel(Args a, int32_t keys) {
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group, i = token - s.q0;
   if (i >= s.n || rows <= kFewRows) return;
-  const int32_t r0 = (i * a.group + head % a.group) / kManyRows * kManyRows;
-  const int32_t parts = parts_of(block_range(a, s, r0, min(r0 + kManyRows, rows) - 1, keys),
+  const int32_t r0 = (i * a.group + head % a.group) / kManyRows<D> * kManyRows<D>;
+  const int32_t parts = parts_of(block_range(a, s, r0, min(r0 + kManyRows<D>, rows) - 1, keys),
                                  a.many_chunk, a.many_splits);
   if (parts == 1) return;
   const int64_t at = ((int64_t)token * a.heads + head) * a.many_splits;
@@ -1028,16 +1171,17 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   if (max_kv < 1) max_kv = 1;
   const int64_t pairs = (int64_t)b.n_seq * c.kv_heads;
   L.many = max_q * group > kFewRows;
+  const int64_t many_rows = c.dim == 256 ? kManyRows<256> : kManyRows<128>;
   int64_t few_keys = max_kv, many_keys = max_kv;
   if (b.window) {
     few_keys = std::min<int64_t>(max_kv, (int64_t)b.window + kFewRows + 32);
-    many_keys = std::min<int64_t>(max_kv, (int64_t)b.window + kManyRows + 64);
+    many_keys = std::min<int64_t>(max_kv, (int64_t)b.window + many_rows + 64);
   }
   split_keys(few_keys, pairs, 1024, 256, 4096, 128, &L.few_splits, &L.few_chunk);
-  L.row_blocks = (int32_t)((int64_t)b.n_tokens * group / kManyRows + b.n_seq);
+  L.row_blocks = (int32_t)((int64_t)b.n_tokens * group / many_rows + b.n_seq);
   // workgroups that have rows: as many as the tokens fill
-  const int64_t full = ceil_div((int64_t)b.n_tokens * group, kManyRows) * c.kv_heads;
-  split_keys(many_keys, full, 512, 256, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
+  const int64_t full = ceil_div((int64_t)b.n_tokens * group, many_rows) * c.kv_heads;
+  split_keys(many_keys, full, 256, 256, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
   if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_splits;
   if (L.many && L.many_splits > 1)
     L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
@@ -1069,7 +1213,7 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   if (few >= (int64_t)1 << 31 || many >= (int64_t)1 << 31)
     return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
   if (L.many) {
-    many_rows_kernel<TYPE, D><<<dim3((uint32_t)many), 256, 0, stream>>>(a);
+    many_rows_kernel<TYPE, D><<<dim3((uint32_t)many), Many<TYPE, D>::threads, 0, stream>>>(a);
     if (int rc = launched()) return rc;
   }
   few_rows_kernel<TYPE, D><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
