@@ -92,6 +92,14 @@ __device__ __forceinline__ Range token_range(const Args &a, const Seq &s, int32_
   return r;
 }
 
+// Of the keys k0 .. k0 + 63 that are there, those within the range, as bits.
+__device__ __forceinline__ uint64_t keys_seen(Range r, int32_t k0, uint64_t there) {
+  auto below = [](int32_t n) {
+    return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+  };
+  return below(r.hi - k0) & ~below(r.lo - k0) & there;
+}
+
 // Keys of the rows r0 .. r1 (inclusive): the first token's first to the last
 // token's last, from a multiple of `unit` on.
 __device__ __forceinline__ Range block_range(const Args &a, const Seq &s, int32_t r0, int32_t r1,
@@ -206,6 +214,20 @@ __device__ __forceinline__ bool take_unbounded(u32x4 &x) {
   }
   return any != 0;
 }
+// The same of fp8 codes, of which 0x7f and 0xff are NaN.
+__device__ __forceinline__ bool take_nan_codes(u32x4 &x) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t seven = x[i] & 0x7f7f7f7fu;
+    const uint32_t top = (seven + 0x01010101u) & 0x80808080u;  // where a byte was 0x7f
+    const uint32_t m = (top >> 7) * 0xffu;
+    any |= m;
+    x[i] &= ~m;
+  }
+  return any != 0;
+}
+
 // Element d of a row of values, if it is not finite; otherwise zero.
 template <int TYPE, int D>
 __device__ __forceinline__ float unbounded_value(const Args &a, int32_t row, int d) {
@@ -235,8 +257,8 @@ __device__ __forceinline__ float natural_lse(float m, float l) {
 //
 // Up to 16 rows (tokens x heads of a group) of a request and KV head: each
 // cached element is read once for all of them, so the cache's bytes bound this.
-// Four waves take 32 keys each in turn, with their own running sums, and join
-// at the end; long requests are split over workgroups too.  Keys go from memory
+// The waves take 32 keys each in turn, with their own running sums, and join at
+// the end; long requests are split over workgroups too.  Keys go from memory
 // into the matrix layout directly; values by way of shared memory, 32 rows a
 // wave, for the transposing read.
 
@@ -245,7 +267,7 @@ constexpr bool kBf = TYPE == WS_KV_BF16;
 template <int TYPE>
 constexpr bool kCodes = TYPE == WS_KV_FP8 || TYPE == WS_KV_INT8;
 
-template <int TYPE, int D>
+template <int TYPE, int D, int W>  // W waves
 struct Few {
   static constexpr int esz = kCodes<TYPE> ? 1 : 2;
   static constexpr int steps = D / 32;            // of the product over d
@@ -257,8 +279,8 @@ struct Few {
   static constexpr int row_bytes = D * 2;         // a row of values in shared memory
   static constexpr int wave_bytes = 32 * row_bytes + 32 * 12;
   static constexpr int join_stride = D + 4;       // floats
-  static constexpr int join_bytes = 4 * 16 * (join_stride + 2) * 4;
-  static constexpr int smem = wave_bytes * 4 > join_bytes ? wave_bytes * 4 : join_bytes;
+  static constexpr int join_bytes = W * 16 * (join_stride + 2) * 4;
+  static constexpr int smem = wave_bytes * W > join_bytes ? wave_bytes * W : join_bytes;
 };
 
 // 16-byte chunk c of key row `key` lies at chunk c ^ few_swizzle(key), which
@@ -268,17 +290,17 @@ __device__ __forceinline__ int few_swizzle(int key) {
   return D == 64 ? ((key >> 1) & 3) << 1 : (key & 7) << 1;
 }
 
-template <int TYPE, int D>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a) {
-  using F = Few<TYPE, D>;
+template <int TYPE, int D, int W>
+__device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) {
+  using F = Few<TYPE, D, W>;
   constexpr bool BF = kBf<TYPE>;
   constexpr bool CODES = kCodes<TYPE>;
-  __shared__ alignas(16) char smem[F::smem];
+  constexpr int stride = 32 * W;  // keys of one turn of the waves
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  const int32_t split = blockIdx.x % a.few_splits;
-  const int32_t at = blockIdx.x / a.few_splits;
+  const int32_t split = id % a.few_splits;
+  const int32_t at = id / a.few_splits;
   const int32_t h = at % a.kv_heads, b = at / a.kv_heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
@@ -368,14 +390,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
     int32_t row_at = kNoRow, next_page = 0;
     if (k0 < end) {
       const int32_t page = page_entry(a, b, k0 + mine, end);
-      next_page = page_entry(a, b, k0 + 128 + mine, end);
+      next_page = page_entry(a, b, k0 + stride + mine, end);
       row_at = cache_row(a, page, h, k0 + mine, end);
       load_keys(row_at);
       load_values(row_at);
     }
-    for (; k0 < end; k0 += 128) {
-      const bool more = k0 + 128 < end;
-      const int32_t next_at = cache_row(a, next_page, h, k0 + 128 + mine, end);
+    for (; k0 < end; k0 += stride) {
+      const bool more = k0 + stride < end;
+      // pages are asked for before the rows behind them, so that waiting for a
+      // page is not waiting for those
+      int32_t next_at = cache_row(a, next_page, h, k0 + stride + mine, end);
+      next_page = page_entry(a, b, k0 + 2 * stride + mine, end);
       const uint32_t there = (uint32_t)__ballot(row_at != kNoRow);
       const bool all = k0 >= lo_all.lo && k0 + 32 <= min(hi_all.hi, end) && there == 0xffffffffu;
       if constexpr (CODES) {
@@ -413,32 +438,31 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
       if (more) load_keys(next_at);
       // values to shared memory; rows that are not there as zeros, because a
       // weight of zero does not take away a NaN
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < F::vloads; ++i) {
+          if (!(there >> (i * F::vrows + lane / F::chunks) & 1)) vreg[i] = u32x4{0, 0, 0, 0};
+          if constexpr (!CODES) bad |= take_unbounded<BF>(vreg[i]);
+          if constexpr (TYPE == WS_KV_FP8) bad |= take_nan_codes(vreg[i]);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < F::vloads; ++i) {
         const int key = i * F::vrows + lane / F::chunks, c = lane % F::chunks;
-        const bool is = there >> key & 1;
-        u32x4 x = vreg[i];
-        if (!is) x = u32x4{0, 0, 0, 0};
+        const u32x4 x = vreg[i];
         char *to = vbuf + key * F::row_bytes;
         const int sw = few_swizzle<D>(key);
         if constexpr (CODES) {
           const u32x2 x0 = codes_to_half<TYPE>(x[0]), x1 = codes_to_half<TYPE>(x[1]);
           const u32x2 x2 = codes_to_half<TYPE>(x[2]), x3 = codes_to_half<TYPE>(x[3]);
-          u32x4 y0 = {x0[0], x0[1], x1[0], x1[1]}, y1 = {x2[0], x2[1], x3[0], x3[1]};
-          if (TYPE == WS_KV_FP8 && !all) {
-            bad |= take_unbounded<BF>(y0);
-            bad |= take_unbounded<BF>(y1);
-          }
-          *reinterpret_cast<u32x4 *>(to + ((2 * c) ^ sw) * 16) = y0;
-          *reinterpret_cast<u32x4 *>(to + ((2 * c + 1) ^ sw) * 16) = y1;
+          *reinterpret_cast<u32x4 *>(to + ((2 * c) ^ sw) * 16) = u32x4{x0[0], x0[1], x1[0], x1[1]};
+          *reinterpret_cast<u32x4 *>(to + ((2 * c + 1) ^ sw) * 16) = u32x4{x2[0], x2[1], x3[0], x3[1]};
         } else {
-          if (!all) bad |= take_unbounded<BF>(x);
           *reinterpret_cast<u32x4 *>(to + (c ^ sw) * 16) = x;
         }
       }
       if (more) load_values(next_at);
       row_at = next_at;
-      next_page = page_entry(a, b, k0 + 256 + mine, end);
 
       float w[8], ref[8], vsc[8];
       if constexpr (CODES) {
@@ -459,12 +483,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
         for (int i = 0; i < 8; ++i) w[i] = z[i / 4][i % 4] * by;
       }
       if (!all) {
+        const uint32_t in = (uint32_t)keys_seen(see, k0, there) >> (4 * g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int j = 16 * (i / 4) + 4 * g + i % 4;
-          const bool in = k0 + j >= see.lo && k0 + j < see.hi && (there >> j & 1);
-          if (!in) w[i] = -INFINITY;
-        }
+        for (int i = 0; i < 8; ++i) w[i] = in & 1u << (16 * (i / 4) + i % 4) ? w[i] : -INFINITY;
       }
       float top = -INFINITY;
 #pragma unroll
@@ -504,7 +525,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
       __builtin_amdgcn_wave_barrier();
     }
     if (__any(bad)) {
-      for (k0 = begin + 32 * wave; k0 < end; k0 += 128) {
+      for (k0 = begin + 32 * wave; k0 < end; k0 += stride) {
         const uint32_t there = (uint32_t)__ballot(
             cache_row(a, page_entry(a, b, k0 + mine, end), h, k0 + mine, end) != kNoRow);
         if (k0 >= lo_all.lo && k0 + 32 <= min(hi_all.hi, end) && there == 0xffffffffu) continue;
@@ -522,9 +543,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
 
-    // the four waves join through shared memory
+    // the waves join through shared memory
     __syncthreads();
-    float *jo = (float *)smem, *jm = jo + 4 * 16 * F::join_stride, *jl = jm + 64;
+    float *jo = (float *)smem, *jm = jo + W * 16 * F::join_stride, *jl = jm + W * 16;
 #pragma unroll
     for (int i = 0; i < F::tiles; ++i)
       *reinterpret_cast<f32x4 *>(jo + (wave * 16 + n16) * F::join_stride + 16 * i + 4 * g) = o[i];
@@ -534,16 +555,16 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
     }
     __syncthreads();
     constexpr int per = D / 4;  // threads of a row, four elements each
-    for (int r = threadIdx.x / per; r <= r1 - r0; r += 256 / per) {
+    for (int r = threadIdx.x / per; r <= r1 - r0; r += 64 * W / per) {
       const int d = threadIdx.x % per * 4;
-      float mw[4], top = -INFINITY;
+      float mw[W], top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, mw[i] = jm[i * 16 + r]);
+      for (int i = 0; i < W; ++i) top = fmaxf(top, mw[i] = jm[i * 16 + r]);
       const float base = top == -INFINITY ? 0.0f : top;
       float total = 0.0f;
       f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < W; ++i) {
         const float e = exp2_of(mw[i] - base);
         total += jl[i * 16 + r] * e;
         x += *reinterpret_cast<const f32x4 *>(jo + (i * 16 + r) * F::join_stride + d) * e;
@@ -566,6 +587,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) few_rows_kernel(Args a)
     }
     __syncthreads();
   }
+}
+
+template <int TYPE, int D, int W>
+__global__ void __launch_bounds__(64 * W, D == 256 ? 1 : 2) few_rows_kernel(Args a) {
+  __shared__ alignas(16) char smem[Few<TYPE, D, W>::smem];
+  few_rows<TYPE, D, W>(a, blockIdx.x, smem);
 }
 
 // ------------------------------------------------------ many rows -------
@@ -641,17 +668,16 @@ __device__ __forceinline__ int value_swizzle(int key) {
 }
 
 template <int TYPE, int D>
-__global__ void __launch_bounds__(D == 256 ? 256 : 512, D == 256 ? 1 : 2) many_rows_kernel(Args a) {
+__device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem) {
   using M = Many<TYPE, D>;
   constexpr bool BF = kBf<TYPE>;
   constexpr bool CODES = kCodes<TYPE>;
-  __shared__ alignas(16) char smem[M::smem];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
   // the blocks of a head that run together read the same keys
-  const int32_t h = blockIdx.x % a.kv_heads;
-  const int32_t work = blockIdx.x / a.kv_heads;
+  const int32_t h = id % a.kv_heads;
+  const int32_t work = id / a.kv_heads;
   const int32_t split = work / a.row_blocks, nth = work % a.row_blocks;
   const int32_t b = last_at_most(a, [&](int32_t i) { return first_block<D>(a, i) <= nth; });
   if (b < 0) return;
@@ -798,13 +824,14 @@ __global__ void __launch_bounds__(D == 256 ? 256 : 512, D == 256 ? 1 : 2) many_r
         const int sw = v ? value_swizzle<D>(key) : key_swizzle<D>(key);
         char *to = smem + tile * M::side + key * M::row_bytes;
         u32x4 x = reg[i];
-        if (!((v ? value_there : key_there) >> key & 1)) x = u32x4{0, 0, 0, 0};
+        if (v && (edge || value_there != ~0ull)) {
+          if (!(value_there >> key & 1)) x = u32x4{0, 0, 0, 0};
+          if (TYPE == WS_KV_FP8) bad |= take_nan_codes(x);
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const u32x2 y = codes_to_half<TYPE>(x[2 * half]), z = codes_to_half<TYPE>(x[2 * half + 1]);
-          u32x4 w = {y[0], y[1], z[0], z[1]};
-          if (TYPE == WS_KV_FP8 && v && edge) bad |= take_unbounded<BF>(w);
-          *reinterpret_cast<u32x4 *>(to + ((2 * c + half) ^ sw) * 16) = w;
+          *reinterpret_cast<u32x4 *>(to + ((2 * c + half) ^ sw) * 16) = u32x4{y[0], y[1], z[0], z[1]};
         }
       }
       if (keys && wave == 0 && lane < M::keys) {
@@ -896,7 +923,6 @@ __global__ void __launch_bounds__(D == 256 ? 256 : 512, D == 256 ? 1 : 2) many_r
       for (int c = 0; c < 2 * M::ktiles; ++c) p[c] = u32x4{0, 0, 0, 0};
       return;
     }
-    const uint32_t there_lo = (uint32_t)there, there_hi = (uint32_t)(there >> 32);
     const bool full = k0 >= every.lo && k0 + M::keys <= min(every.hi, end) && there == ~0ull;
     const float *sc = (const float *)(smem + 4 * M::side + (t & 1) * M::scales);
     auto scales = [&](int which, int k, int r4) {
@@ -913,15 +939,13 @@ __global__ void __launch_bounds__(D == 256 ? 256 : 512, D == 256 ? 1 : 2) many_r
         }
     }
     if (!full) {
+      const uint64_t in = keys_seen(see, k0, there) >> (4 * hh);
+      const uint32_t half[2] = {(uint32_t)in, (uint32_t)(in >> 32)};
 #pragma unroll
       for (int k = 0; k < M::ktiles; ++k)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = 8 * (r / 4) + 4 * hh + r % 4;
-          const int32_t key = k0 + 32 * k + j;
-          const bool in = (key >= see.lo) & (key < see.hi) & ((k ? there_hi : there_lo) >> j & 1);
-          z[k][r] = in ? z[k][r] : -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r)
+          z[k][r] = half[k] & 1u << (8 * (r / 4) + r % 4) ? z[k][r] : -INFINITY;
     }
     // the largest score, times log2(e) and the scale; of codes, plus log2 of the
     // value's scale
@@ -1071,41 +1095,75 @@ __global__ void __launch_bounds__(D == 256 ? 256 : 512, D == 256 ? 1 : 2) many_r
   }
 }
 
+// A batch of both kinds in one launch: the long workgroups first, the others
+// where these leave room.
+template <int D>
+constexpr int kWideWaves = D == 256 ? 4 : 8;
+
+template <int TYPE, int D>
+__global__ void __launch_bounds__(64 * kWideWaves<D>, D == 256 ? 1 : 2) rows_kernel(Args a, int32_t many) {
+  constexpr int few_smem = Few<TYPE, D, kWideWaves<D>>::smem, many_smem = Many<TYPE, D>::smem;
+  __shared__ alignas(16) char smem[few_smem > many_smem ? few_smem : many_smem];
+  if ((int32_t)blockIdx.x < many)
+    many_rows<TYPE, D>(a, blockIdx.x, smem);
+  else
+    few_rows<TYPE, D, kWideWaves<D>>(a, blockIdx.x - many, smem);
+}
+
 // ----------------------------------------------------------- joining ----
 //
 // A wave joins the parts of one (token, head), D / 64 elements a lane.
 
 template <int D>
-__device__ __forceinline__ void join_parts(const Args &a, const float *part_o, const float2 *part_ml,
-                                           int32_t parts, int64_t q_row, int32_t head) {
+struct Joined {
+  float o[D / 64];
+  float m, l;
+};
+
+template <int D>
+__device__ __forceinline__ Joined<D> join_parts(const float *part_o, const float2 *part_ml,
+                                                int32_t first, int32_t step, int32_t parts) {
   constexpr int per = D / 64;
   const int lane = threadIdx.x & 63;
-  float top = -INFINITY;
-  for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, part_ml[k].x);
+  Joined<D> j;
+  j.m = -INFINITY;
+  for (int32_t k = first + step * lane; k < parts; k += 64 * step) j.m = fmaxf(j.m, part_ml[k].x);
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-  const float base = top == -INFINITY ? 0.0f : top;
-  float total = 0.0f, o[per] = {};
-#pragma unroll 8
-  for (int32_t k = 0; k < parts; ++k) {
+  for (int x = 1; x < 64; x *= 2) j.m = fmaxf(j.m, __shfl_xor(j.m, x));
+  const float base = j.m == -INFINITY ? 0.0f : j.m;
+  j.l = 0.0f;
+#pragma unroll
+  for (int i = 0; i < per; ++i) j.o[i] = 0.0f;
+#pragma unroll 4
+  for (int32_t k = first; k < parts; k += step) {
     const float2 ml = part_ml[k];
     const float e = exp2_of(ml.x - base);
-    total += ml.y * e;
+    j.l += ml.y * e;
 #pragma unroll
-    for (int j = 0; j < per; ++j) o[j] += part_o[(int64_t)k * D + lane * per + j] * e;
+    for (int i = 0; i < per; ++i) j.o[i] += part_o[(int64_t)k * D + lane * per + i] * e;
   }
-  const float inv = safe_inverse(total);
-  uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + lane * per;
-#pragma unroll
-  for (int j = 0; j < per; ++j) p[j] = out_bits(a, o[j] * inv);
-  if (a.lse && lane == 0) a.lse[q_row * a.heads + head] = natural_lse(top, total);
+  return j;
 }
 
 template <int D>
+__device__ __forceinline__ void put_joined(const Args &a, const Joined<D> &j, int64_t q_row,
+                                           int32_t head) {
+  constexpr int per = D / 64;
+  const int lane = threadIdx.x & 63;
+  const float inv = safe_inverse(j.l);
+  uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + lane * per;
+#pragma unroll
+  for (int i = 0; i < per; ++i) p[i] = out_bits(a, j.o[i] * inv);
+  if (a.lse && lane == 0) a.lse[q_row * a.heads + head] = natural_lse(j.m, j.l);
+}
+
+// Few rows have many parts: four waves share a (request, head).
+template <int D>
 __global__ void __launch_bounds__(256) join_few_kernel(Args a) {
-  const int32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int32_t head = id % a.heads, b = id / a.heads;
-  if (b >= a.n_seq) return;
+  constexpr int per = D / 64;
+  __shared__ Joined<D> shared[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t head = blockIdx.x % a.heads, b = blockIdx.x / a.heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
   if (rows == 0 || rows > kFewRows) return;
@@ -1114,7 +1172,23 @@ __global__ void __launch_bounds__(256) join_few_kernel(Args a) {
   const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * kFewRows;
   for (int32_t i = 0; i < s.n; ++i) {
     const int64_t at = (from + i * a.group + head % a.group) * a.few_splits;
-    join_parts<D>(a, a.few_o + at * D, a.few_ml + at, parts, s.q0 + i, head);
+    shared[wave][lane] = join_parts<D>(a.few_o + at * D, a.few_ml + at, wave, 4, parts);
+    __syncthreads();
+    if (wave == 0) {
+      Joined<D> j = shared[0][lane];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const Joined<D> x = shared[w][lane];
+        const float top = fmaxf(j.m, x.m), base = top == -INFINITY ? 0.0f : top;
+        const float ej = exp2_of(j.m - base), ex = exp2_of(x.m - base);
+        j.m = top;
+        j.l = j.l * ej + x.l * ex;
+#pragma unroll
+        for (int k = 0; k < per; ++k) j.o[k] = j.o[k] * ej + x.o[k] * ex;
+      }
+      put_joined<D>(a, j, s.q0 + i, head);
+    }
+    __syncthreads();
   }
 }
 
@@ -1133,14 +1207,14 @@ __global__ void __launch_bounds__(256) join_many_kernel(Args a, int32_t keys) {
                                  a.many_chunk, a.many_splits);
   if (parts == 1) return;
   const int64_t at = ((int64_t)token * a.heads + head) * a.many_splits;
-  join_parts<D>(a, a.many_o + at * D, a.many_ml + at, parts, token, head);
+  put_joined<D>(a, join_parts<D>(a.many_o + at * D, a.many_ml + at, 0, 1, parts), token, head);
 }
 
 // -------------------------------------------------------------- host -----
 
 // How a batch is laid out over workgroups.
 struct Layout {
-  bool many;
+  bool many, wide;
   int32_t few_splits, few_chunk, many_splits, many_chunk, row_blocks;
   int64_t few_slots, many_slots;  // results of parts in the workspace
   int64_t bytes;
@@ -1177,7 +1251,11 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
     few_keys = std::min<int64_t>(max_kv, (int64_t)b.window + kFewRows + 32);
     many_keys = std::min<int64_t>(max_kv, (int64_t)b.window + many_rows + 64);
   }
-  split_keys(few_keys, pairs, 1024, 256, 4096, 128, &L.few_splits, &L.few_chunk);
+  // Few rows: with a workgroup of four waves and 512 of them at once the card is
+  // full; below that eight waves share a pair, one workgroup a CU.
+  L.wide = L.many || pairs < 512;
+  split_keys(few_keys, pairs, L.wide ? 256 : 512, L.wide ? 1024 : 512, 4096, 256, &L.few_splits,
+             &L.few_chunk);
   L.row_blocks = (int32_t)((int64_t)b.n_tokens * group / many_rows + b.n_seq);
   // workgroups that have rows: as many as the tokens fill
   const int64_t full = ceil_div((int64_t)b.n_tokens * group, many_rows) * c.kv_heads;
@@ -1200,9 +1278,10 @@ int check_batch(const ws_kv_cache *c, const ws_kv_batch *b) {
   if (b->window < 0) return invalid("attention: the window must not be negative");
   if (b->max_q_len < 0 || b->max_kv_len < 0) return invalid("attention: bad length bounds");
   if ((int64_t)b->n_tokens * b->heads >= (int64_t)1 << 31 ||
+      (int64_t)b->n_seq * b->heads >= (int64_t)1 << 31 ||
       (int64_t)b->table_cols * c->page_size >= (int64_t)1 << 30)
     return ws_record_failure(WS_EUNSUPPORTED,
-                             "attention: 2^31 rows or 2^30 keys a request, or more");
+                             "attention: 2^31 rows or requests times heads, or 2^30 keys a request");
   return WS_OK;
 }
 
@@ -1212,14 +1291,19 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   const int64_t few = pairs * L.few_splits, many = (int64_t)a.kv_heads * L.many_splits * L.row_blocks;
   if (few >= (int64_t)1 << 31 || many >= (int64_t)1 << 31)
     return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
+  constexpr int wide = kWideWaves<D>;
   if (L.many) {
-    many_rows_kernel<TYPE, D><<<dim3((uint32_t)many), Many<TYPE, D>::threads, 0, stream>>>(a);
-    if (int rc = launched()) return rc;
+    if (few + many >= (int64_t)1 << 31)
+      return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
+    rows_kernel<TYPE, D><<<dim3((uint32_t)(few + many)), 64 * wide, 0, stream>>>(a, (int32_t)many);
+  } else if (L.wide) {
+    few_rows_kernel<TYPE, D, wide><<<dim3((uint32_t)few), 64 * wide, 0, stream>>>(a);
+  } else {
+    few_rows_kernel<TYPE, D, 4><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
   }
-  few_rows_kernel<TYPE, D><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
   if (int rc = launched()) return rc;
   if (L.few_slots) {
-    join_few_kernel<D><<<dim3((uint32_t)ceil_div((int64_t)a.n_seq * a.heads, 4)), 256, 0, stream>>>(a);
+    join_few_kernel<D><<<dim3((uint32_t)(a.n_seq * a.heads)), 256, 0, stream>>>(a);
     if (int rc = launched()) return rc;
   }
   if (L.many_slots)
