@@ -143,7 +143,8 @@ __device__ __forceinline__ void load_n(const typename T::raw *p, float (&x)[N]) 
     for (int j = 0; j < VEC; ++j) x[i + j] = T::get(v.r[j]);
   }
 }
-template <class T, int N, int VEC>
+// STREAM: past the caches, for outputs that these cannot hold.
+template <class T, int N, int VEC, bool STREAM = false>
 __device__ __forceinline__ void store_n(typename T::raw *p, const float (&x)[N]) {
   struct alignas(VEC * sizeof(typename T::raw)) Pack {
     typename T::raw r[VEC];
@@ -153,7 +154,10 @@ __device__ __forceinline__ void store_n(typename T::raw *p, const float (&x)[N])
     Pack v;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) v.r[j] = T::put(x[i + j]);
-    *reinterpret_cast<Pack *>(p + i) = v;
+    if constexpr (STREAM && sizeof(Pack) == 16)
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(p + i));
+    else
+      *reinterpret_cast<Pack *>(p + i) = v;
   }
 }
 
