@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(64 * W, D == 256 ? 1 : 2) few_rows_kernel(Args
 // for the scheduler: kinds of instructions, and products whose operands are read
 // ahead
 constexpr int kMatrix = 0x8, kLdsRead = 0x100;
-constexpr int kAhead = 6;
+constexpr int kAhead = 3;
 
 template <int D>
 constexpr int kManyRows = D == 256 ? 128 : 256;
@@ -864,56 +864,53 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
   // 4 hh + r % 4.  Their weights p[c]: keys 16 c + 4 hh + (0..3) and + 8.
   f32x16 z[M::ktiles];
   u32x4 p[2 * M::ktiles];
-  auto add_values = [&](int32_t t) {
-    const char *vb = smem + (2 + (t & 1)) * M::side;
+  // Product number e of the values of tile t, and of the scores: each has as many
+  // as the other.
+  constexpr int products = 2 * M::ktiles * M::tiles;
+  static_assert(products == M::ktiles * M::steps, "");
+  auto value_product = [&](int32_t t, int e) {
+    const int c = e / M::tiles, i = e % M::tiles;
     const int i16 = lane & 15, q2 = (lane >> 4) & 1;
     const int key = 4 * hh + i16 / 4;
     const int sw = value_swizzle<D>(key);  // the same for key + 8, + 16, ...
-    const char *v0 = vb + key * M::row_bytes + (i16 & 1) * 8;
+    const char *at = smem + (2 + (t & 1)) * M::side + key * M::row_bytes + (i16 & 1) * 8 +
+                     ((4 * i + 2 * q2 + ((i16 & 3) >> 1)) ^ sw) * 16 + 16 * c * M::row_bytes;
+    const u32x2 x = read_column(at), y = read_column(at + 8 * M::row_bytes);
+    o[i] = mfma32<BF>(u32x4{x[0], x[1], y[0], y[1]}, p[c], o[i]);
+  };
+  auto score_product = [&](int32_t t, int e) {
+    const int i = e / M::ktiles, k = e % M::ktiles;
+    const int sw = key_swizzle<D>(n32);  // the same for key + 32
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(
+        smem + (t & 1) * M::side + (n32 + 32 * k) * M::row_bytes + ((2 * i + hh) ^ sw) * 16);
+    if (i == 0) z[k] = f32x16{};
+    z[k] = mfma32<BF>(x, q[i], z[k]);
+  };
+  auto add_values = [&](int32_t t) {
 #pragma unroll
-    for (int c = 0; c < 2 * M::ktiles; ++c) {
-#pragma unroll
-      for (int i = 0; i < M::tiles; ++i) {
-        const char *at = v0 + ((4 * i + 2 * q2 + ((i16 & 3) >> 1)) ^ sw) * 16 + 16 * c * M::row_bytes;
-        const u32x2 x = read_column(at), y = read_column(at + 8 * M::row_bytes);
-        o[i] = mfma32<BF>(u32x4{x[0], x[1], y[0], y[1]}, p[c], o[i]);
-      }
-    }
+    for (int e = 0; e < products; ++e) value_product(t, e);
   };
   auto score = [&](int32_t t) {
-    const char *kb = smem + (t & 1) * M::side + n32 * M::row_bytes;
-    const int sw = key_swizzle<D>(n32);  // the same for key + 32
 #pragma unroll
-    for (int k = 0; k < M::ktiles; ++k) z[k] = f32x16{};
-#pragma unroll
-    for (int i = 0; i < M::steps; ++i) {
-#pragma unroll
-      for (int k = 0; k < M::ktiles; ++k) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(kb + 32 * k * M::row_bytes +
-                                                         ((2 * i + hh) ^ sw) * 16);
-        z[k] = mfma32<BF>(x, q[i], z[k]);
-      }
-    }
+    for (int e = 0; e < products; ++e) score_product(t, e);
   };
-  // Products run 32 cycles each, a read from shared memory takes a few times
-  // that: kAhead products' reads are under way before the first.
+  // Both, in turn, so that a product does not wait for the one before it.  They
+  // run 32 cycles each, a read from shared memory takes a few times that: the
+  // reads of kAhead pairs are under way before the first.
   auto multiply = [&](int32_t t) {
     __builtin_amdgcn_s_setprio(1);
-    add_values(t - 1);
-    score(t);
-    constexpr int pv = 2 * M::ktiles * M::tiles, qk = M::ktiles * M::steps;
-    __builtin_amdgcn_sched_group_barrier(kLdsRead, 2 * kAhead, 0);
 #pragma unroll
-    for (int i = 0; i < pv - kAhead; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
+    for (int e = 0; e < products; ++e) {
+      value_product(t - 1, e);
+      score_product(t, e);
     }
+    __builtin_amdgcn_sched_group_barrier(kLdsRead, 3 * kAhead, 0);
 #pragma unroll
-    for (int i = 0; i < qk; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
+    for (int e = 0; e < products - kAhead; ++e) {
+      __builtin_amdgcn_sched_group_barrier(kMatrix, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kLdsRead, 3, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead, 0);
+    __builtin_amdgcn_sched_group_barrier(kMatrix, 2 * kAhead, 0);
     __builtin_amdgcn_s_setprio(0);
   };
   auto weigh = [&](int32_t t, uint64_t there) {
@@ -991,6 +988,10 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
     }
   };
 
+  auto turn = [] {
+    if constexpr (M::groups > 1) __syncthreads();
+  };
+
   if (n > 0) {
     ask(0);
     const int32_t first = find(0, key_there);
@@ -1009,7 +1010,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
     load(0, n > 1, true);
     if (M::groups == 1 || wave < 4) {
       score(0);
-      __syncthreads();
+      turn();
       weigh(0, value_there);
       arrive(0, n > 1, true);
       look(0);
@@ -1017,14 +1018,14 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
       for (int32_t t = 1; t < n; ++t) {
         load(t, t + 1 < n, true);
         multiply(t);
-        __syncthreads();
+        turn();
         weigh(t, value_there);
         arrive(t, t + 1 < n, true);
         look(t);
         __syncthreads();
       }
     } else {
-      __syncthreads();
+      turn();
       score(0);
       arrive(0, n > 1, true);
       look(0);
@@ -1032,7 +1033,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
       for (int32_t t = 1; t < n; ++t) {
         load(t, t + 1 < n, true);
         weigh(t - 1, there_before);
-        __syncthreads();
+        turn();
         multiply(t);
         arrive(t, t + 1 < n, true);
         look(t);
