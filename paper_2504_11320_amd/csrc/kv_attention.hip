@@ -40,17 +40,18 @@ struct Args {
   float scale;  // times log2(e)
   int32_t causal, window;
   int32_t q_bf16;
-  // results of parts, the sums o and (m, l): few rows [request][KV head][16]
-  // [part], many rows [token][head][part]
+  // results of parts, the sums o and (m, l): few rows [request][KV head]
+  // [few_blocks * 16][part], many rows [token][head][part]
   float *few_o, *many_o;
   float2 *few_ml, *many_ml;
   int32_t few_splits, few_chunk;    // of a few-rows launch: parts, keys a part
+  int32_t few_blocks;               // and row blocks of a request
   int32_t many_splits, many_chunk;  // of a many-rows launch
-  int32_t both;          // requests of more than 16 rows are the other launch's
+  int32_t both;          // requests of more than 16 rows are the many-rows blocks'
   int32_t row_blocks;    // numbers of row blocks of the many-rows launch
 };
 
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 16;  // of a few-rows block
 
 // The queries of request b and its keys.
 struct Seq {
@@ -118,7 +119,7 @@ __device__ __forceinline__ int32_t parts_of(Range r, int32_t chunk, int32_t spli
 // The parts of a few-rows block.  A request that has more rows than its launch
 // was laid out for has no room for parts.
 __device__ __forceinline__ int32_t few_parts(const Args &a, Range r, int32_t rows) {
-  return rows > kFewRows ? 1 : parts_of(r, a.few_chunk, a.few_splits);
+  return rows > kFewRows * a.few_blocks ? 1 : parts_of(r, a.few_chunk, a.few_splits);
 }
 
 // Key j of a request, 0 < end: its page's entry in the table, read ahead (the
@@ -299,8 +300,12 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
+  // the row blocks of a request and head follow one another: they read the same
+  // keys at about the same time
   const int32_t split = id % a.few_splits;
-  const int32_t at = id / a.few_splits;
+  int32_t at = id / a.few_splits;
+  const int32_t first = at % a.few_blocks * kFewRows;
+  at /= a.few_blocks;
   const int32_t h = at % a.kv_heads, b = at / a.kv_heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
@@ -309,7 +314,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
   char *vbuf = smem + wave * F::wave_bytes;
   float *kscale = (float *)(vbuf + 32 * F::row_bytes), *vlog = kscale + 32, *vscale = vlog + 32;
 
-  for (int32_t r0 = 0; r0 < rows; r0 += kFewRows) {
+  for (int32_t r0 = first; r0 < rows; r0 += kFewRows * a.few_blocks) {
     const int32_t r1 = min(r0 + kFewRows, rows) - 1;
     const Range block = block_range(a, s, r0, r1, 32);
     const int32_t parts = few_parts(a, block, rows);
@@ -580,7 +585,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         if (a.lse && d == 0) a.lse[q_row * a.heads + hd] = natural_lse(top, total);
       } else {
         const int64_t to =
-            ((int64_t)(b * a.kv_heads + h) * kFewRows + r) * a.few_splits + split;
+            ((int64_t)(b * a.kv_heads + h) * a.few_blocks * kFewRows + r0 + r) * a.few_splits + split;
         *reinterpret_cast<f32x4 *>(a.few_o + to * D + d) = x;
         if (d == 0) a.few_ml[to] = make_float2(top, total);
       }
@@ -1167,12 +1172,14 @@ __global__ void __launch_bounds__(256) join_few_kernel(Args a) {
   const int32_t head = blockIdx.x % a.heads, b = blockIdx.x / a.heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
-  if (rows == 0 || rows > kFewRows) return;
-  const int32_t parts = few_parts(a, block_range(a, s, 0, rows - 1, 32), rows);
-  if (parts == 1) return;
-  const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * kFewRows;
-  for (int32_t i = 0; i < s.n; ++i) {
-    const int64_t at = (from + i * a.group + head % a.group) * a.few_splits;
+  if (rows == 0 || rows > kFewRows * a.few_blocks) return;
+  const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * a.few_blocks * kFewRows;
+  for (int32_t i = blockIdx.y; i < s.n; i += gridDim.y) {
+    const int32_t row = i * a.group + head % a.group, r0 = row / kFewRows * kFewRows;
+    const int32_t parts =
+        few_parts(a, block_range(a, s, r0, min(r0 + kFewRows, rows) - 1, 32), rows);
+    if (parts == 1) continue;
+    const int64_t at = (from + row) * a.few_splits;
     shared[wave][lane] = join_parts<D>(a.few_o + at * D, a.few_ml + at, wave, 4, parts);
     __syncthreads();
     if (wave == 0) {
@@ -1216,7 +1223,7 @@ __global__ void __launch_bounds__(256) join_many_kernel(Args a, int32_t keys) {
 // How a batch is laid out over workgroups.
 struct Layout {
   bool many, wide;
-  int32_t few_splits, few_chunk, many_splits, many_chunk, row_blocks;
+  int32_t few_splits, few_chunk, few_blocks, many_splits, many_chunk, row_blocks;
   int64_t few_slots, many_slots;  // results of parts in the workspace
   int64_t bytes;
 };
@@ -1245,7 +1252,14 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   max_kv = max_kv > capacity ? capacity : max_kv;
   if (max_kv < 1) max_kv = 1;
   const int64_t pairs = (int64_t)b.n_seq * c.kv_heads;
-  L.many = max_q * group > kFewRows;
+  const int64_t max_rows = max_q * group;
+  // Blocks of 16 rows read the keys again, out of a cache where they run at the
+  // same time; up to four of them are quicker than one block of 256 rows over
+  // many keys: 16 requests of 10 to 16 tokens, 4 heads a KV head, over 1000 to
+  // 2000 keys in fp8 39 us against 57, of 5 to 8 tokens 25 against 53.  Over few
+  // keys they are not: 32 prompts of 30 to 60 tokens 47 us against 33.
+  L.many = max_rows > 4 * kFewRows || (max_rows > kFewRows && max_kv < 16 * max_rows);
+  L.few_blocks = L.many ? 1 : (int32_t)ceil_div(max_rows, kFewRows);
   const int64_t many_rows = c.dim == 256 ? kManyRows<256> : kManyRows<128>;
   int64_t few_keys = max_kv, many_keys = max_kv;
   if (b.window) {
@@ -1254,14 +1268,15 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   }
   // Few rows: with a workgroup of four waves and 512 of them at once the card is
   // full; below that eight waves share a pair, one workgroup a CU.
-  L.wide = L.many || pairs < 512;
-  split_keys(few_keys, pairs, L.wide ? 256 : 512, L.wide ? 1024 : 512, 4096, 256, &L.few_splits,
+  const int64_t few_groups = pairs * L.few_blocks;
+  L.wide = L.many || few_groups < 512;
+  split_keys(few_keys, few_groups, L.wide ? 256 : 512, L.wide ? 1024 : 512, 4096, 256, &L.few_splits,
              &L.few_chunk);
   L.row_blocks = (int32_t)((int64_t)b.n_tokens * group / many_rows + b.n_seq);
   // workgroups that have rows: as many as the tokens fill
   const int64_t full = ceil_div((int64_t)b.n_tokens * group, many_rows) * c.kv_heads;
-  split_keys(many_keys, full, 256, 256, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
-  if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_splits;
+  split_keys(many_keys, full, 256, 512, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
+  if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_blocks * L.few_splits;
   if (L.many && L.many_splits > 1)
     L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
   L.bytes = (L.few_slots + L.many_slots) * (c.dim + 2) * 4;
@@ -1289,7 +1304,7 @@ int check_batch(const ws_kv_cache *c, const ws_kv_batch *b) {
 template <int TYPE, int D>
 int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
-  const int64_t few = pairs * L.few_splits, many = (int64_t)a.kv_heads * L.many_splits * L.row_blocks;
+  const int64_t few = pairs * L.few_splits * L.few_blocks, many = (int64_t)a.kv_heads * L.many_splits * L.row_blocks;
   if (few >= (int64_t)1 << 31 || many >= (int64_t)1 << 31)
     return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
   constexpr int wide = kWideWaves<D>;
@@ -1304,7 +1319,8 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   }
   if (int rc = launched()) return rc;
   if (L.few_slots) {
-    join_few_kernel<D><<<dim3((uint32_t)(a.n_seq * a.heads)), 256, 0, stream>>>(a);
+    const int32_t tokens = std::max(1, L.few_blocks * kFewRows / a.group);  // a request has
+    join_few_kernel<D><<<dim3((uint32_t)(a.n_seq * a.heads), tokens), 256, 0, stream>>>(a);
     if (int rc = launched()) return rc;
   }
   if (L.many_slots)
@@ -1392,6 +1408,7 @@ int wait_kv_attention(const ws_kv_cache *cache, const ws_kv_batch *batch, const 
     }
     a.few_splits = L.few_splits;
     a.few_chunk = L.few_chunk;
+    a.few_blocks = L.few_blocks;
     a.many_splits = L.many_splits;
     a.many_chunk = L.many_chunk;
     a.both = L.many;
