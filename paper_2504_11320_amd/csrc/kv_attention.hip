@@ -370,7 +370,12 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
 
     u32x4 kreg[2][F::kloads], vreg[F::vloads];
     float ks = 0.0f, vs = 0.0f;
+    // scales first: they are waited for first
     auto load_keys = [&](int32_t at_row) {
+      if constexpr (CODES) {
+        ks = a.ks[max(at_row, 0)];
+        vs = a.vs[max(at_row, 0)];
+      }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int64_t r = max(__shfl(at_row, 16 * t + n16), 0);
@@ -379,7 +384,6 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         for (int i = 0; i < F::kloads; ++i)
           kreg[t][i] = *reinterpret_cast<const u32x4 *>(p + 64 * i);
       }
-      if constexpr (CODES) ks = a.ks[max(at_row, 0)];
     };
     auto load_values = [&](int32_t at_row) {
 #pragma unroll
@@ -387,7 +391,6 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         const int64_t r = max(__shfl(at_row, i * F::vrows + lane / F::chunks), 0);
         vreg[i] = *reinterpret_cast<const u32x4 *>(a.v + r * (D * F::esz) + 16 * (lane % F::chunks));
       }
-      if constexpr (CODES) vs = a.vs[max(at_row, 0)];
     };
 
     int32_t k0 = begin + 32 * wave;

@@ -58,15 +58,16 @@ def _stream(index: int) -> int:
     return torch.cuda.current_stream(index).cuda_stream
 
 
-# the same without building a Stream object, where this PyTorch has it
+# the same without building objects, where this PyTorch has them
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _run(fn, index: int, *args):
     """fn(*args, the current stream) on GPU number `index`."""
     if index < 0:
         raise ValueError("the operators run on the GPU")
-    if torch.cuda.current_device() == index:
+    if _current() == index:
         rc = fn(*args, _stream(index))
     else:
         with torch.cuda.device(index):
@@ -90,6 +91,12 @@ def _rows(t: torch.Tensor, name: str, index: int, types=_WIDE) -> bytes:
         _need(step[2] == 1 or t.shape[2] == 1, f"{name}: a vector's elements must be contiguous")
         _need(t.get_device() == index, f"{name} must be on the same device, is on {t.device}")
     return ROWS.pack(t.data_ptr(), step[0], step[1], _TYPE[dtype])
+
+
+def _fresh(t: torch.Tensor) -> bytes:
+    """The struct of a contiguous tensor made here."""
+    _, heads, dim = t.shape
+    return ROWS.pack(t.data_ptr(), heads * dim, dim, _TYPE[t.dtype])
 
 
 def _apart(t: torch.Tensor, name: str):
@@ -203,19 +210,19 @@ class Cache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
         size, dtype, index = k.shape, k.dtype, k.get_device()
-        _need(len(size) == 4 and size == v.shape and dtype is v.dtype,
-              "k and v must both be [pages, kv_heads, page_size, dim] of one type")
-        _need(dtype in CACHE_TYPES, f"a cache's type is one of {CACHE_TYPES}")
-        _need(k.is_contiguous() and v.is_contiguous(), "k and v must be contiguous")
-        _need(v.get_device() == index, "k and v must be on one device")
+        if (len(size) != 4 or size != v.shape or dtype is not v.dtype or dtype not in CACHE_TYPES
+                or not k.is_contiguous() or not v.is_contiguous() or v.get_device() != index):
+            raise ValueError("k and v must both be [pages, kv_heads, page_size, dim] of one of "
+                             f"{CACHE_TYPES}, contiguous, on one device")
         kp = vp = 0
         if dtype in EIGHT_BIT:
             _need(k_scale is not None and v_scale is not None, "an 8-bit cache needs scales")
+            rows = size[:3]
             for t in (k_scale, v_scale):
-                _need(t.shape == size[:3] and t.dtype is torch.float32 and t.is_contiguous()
-                      and t.get_device() == index,
-                      "scales must be [pages, kv_heads, page_size], fp32, contiguous, on the "
-                      "cache's device")
+                if (t.shape != rows or t.dtype is not torch.float32 or not t.is_contiguous()
+                        or t.get_device() != index):
+                    raise ValueError("scales must be [pages, kv_heads, page_size], fp32, "
+                                     "contiguous, on the cache's device")
             kp, vp = k_scale.data_ptr(), v_scale.data_ptr()
         else:
             _need(k_scale is None and v_scale is None, "a 16-bit cache has no scales")
@@ -278,15 +285,17 @@ def read(cache: Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
     shape = (n, cache.kv_heads, cache.dim)
     if out is None:
         _need(dtype in _WIDE, f"dtype must be one of {_WIDE}")
-        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        k = torch.empty(*shape, dtype=dtype, device=cache.device)
         v = torch.empty_like(k)
+        kr, vr = _fresh(k), _fresh(v)
     else:
         k, v = out
         _need(k.shape == shape and v.shape == shape and k.dtype is v.dtype,
               "out must be two [slots, kv_heads, dim] of one type")
         _apart(k, "k")
         _apart(v, "v")
-    _run(fn, index, cache._c, slots.data_ptr(), n, _rows(k, "k", index), _rows(v, "v", index))
+        kr, vr = _rows(k, "k", index), _rows(v, "v", index)
+    _run(fn, index, cache._c, slots.data_ptr(), n, kr, vr)
     return k, v
 
 
