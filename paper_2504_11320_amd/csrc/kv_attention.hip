@@ -1278,7 +1278,11 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   L.row_blocks = (int32_t)((int64_t)b.n_tokens * group / many_rows + b.n_seq);
   // workgroups that have rows: as many as the tokens fill
   const int64_t full = ceil_div((int64_t)b.n_tokens * group, many_rows) * c.kv_heads;
-  split_keys(many_keys, full, 256, 512, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
+  // Joining costs by the rows, so many of them take longer parts: a prompt of 512
+  // over 32 heads 28 us with parts of 512 keys and 33 with 256; a prompt of 1024
+  // over 4 heads 31 us with 512 and 25 with 256.  D = 256 has tiles of 32 keys.
+  const int64_t least = (full >= 64 ? 512 : 256) / (c.dim == 256 ? 2 : 1);
+  split_keys(many_keys, full, 256, least, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
   if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_blocks * L.few_splits;
   if (L.many && L.many_splits > 1)
     L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
