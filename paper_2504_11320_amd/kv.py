@@ -192,8 +192,11 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *,
     else:
         _need(out.shape == x.shape and out.dtype == x.dtype, "out must have x's shape and type")
         _apart(out, "out")
+        _rows(out, "out", index)
     if n and heads:
-        _run(fn, index, xr, _rows(out, "out", index), n, heads, dim, t, inverse)
+        step = out.stride()
+        _run(fn, index, xr, ROWS.pack(out.data_ptr(), step[0], step[1], _TYPE[out.dtype]), n, heads,
+             dim, t, inverse)
     return out
 
 
@@ -369,7 +372,8 @@ def _batch(size, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, ca
     cap = cols * cache.page_size
     b = BATCH.pack(pages.data_ptr(), step[0] if n_seq > 1 else cols, cols, starts.data_ptr(),
                    kv_lens.data_ptr(), n_seq, T, heads,
-                   1.0 / math.sqrt(dim) if scale is None else scale, bool(causal), window,
+                   1.0 / math.sqrt(dim) if scale is None else scale, bool(causal),
+                   min(window, 0x7fffffff),
                    T if max_q_len is None else min(max_q_len, T),
                    cap if max_kv_len is None else min(max_kv_len, cap))
     need = C.c_size_t()
