@@ -1,12 +1,14 @@
 """Build the HIP library (gfx950) in-tree: paper_2504_11320_amd/libwait_sim.so.
 
 Each source is compiled to an object in parallel, then the objects are
-linked into one shared library."""
+linked into one shared library.  Beside it comes _kv.so, the Python module
+with the argument checks of the KV-path operators (host code over PyTorch)."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 import time
 from concurrent.futures import ThreadPoolExecutor
@@ -20,6 +22,7 @@ SRC_NAMES = ("wait_sim_host.hip", "sim_wait.hip", "sim_fcfs.hip",
 SRCS = [os.path.join(CSRC, f) for f in SRC_NAMES]
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libwait_sim.so")
+BINDING = os.path.join(PKG, "_kv.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -63,11 +66,27 @@ SANITIZE_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitiz
                   "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-g"]
 
 
+def build_binding(verbose: bool = False, out: str = BINDING) -> str:
+    """Compile the module of csrc/kv_binding.cpp against the installed PyTorch."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INC,
+           "-I", sysconfig.get_path("include"), "-isystem", os.path.join(at, "include"),
+           "-o", out + ".tmp", os.path.join(CSRC, "kv_binding.cpp"),
+           "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    os.replace(out + ".tmp", out)
+    return out
+
+
 def build(verbose: bool = False, defines=(), out: str = LIB, sanitize: bool = False) -> str:
     """Compile every source for gfx950 and link `out` (default: the in-tree
-    library).  `defines` are extra -D options; `sanitize` instruments the host
-    code with ASan and UBSan (load the result with the clang ASan runtime
-    preloaded)."""
+    library; then the module beside it is compiled too).  `defines` are extra
+    -D options; `sanitize` instruments the host code with ASan and UBSan (load
+    the result with the clang ASan runtime preloaded)."""
     dflags = [f"-D{d}" for d in defines] + (SANITIZE_FLAGS if sanitize else [])
     with tempfile.TemporaryDirectory(prefix="wait_sim_build_") as tmp:
         def compile_one(src: str):
@@ -83,7 +102,10 @@ def build(verbose: bool = False, defines=(), out: str = LIB, sanitize: bool = Fa
 
         workers = max(1, min(len(SRCS), os.cpu_count() or 1))
         with ThreadPoolExecutor(workers) as ex:
+            beside = ex.submit(build_binding, verbose) if out == LIB else None
             objs = list(ex.map(compile_one, SRCS))
+            if beside:
+                beside.result()
         cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out + ".tmp"] + objs
         if sanitize:
             cmd += ["-fsanitize=address,undefined", "-shared-libasan"]

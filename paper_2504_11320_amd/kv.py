@@ -1,6 +1,6 @@
 """The KV path of one serving iteration on the card: Python side of
-include/wait_kv.h (argument checks and marshalling; PyTorch allocates buffers
-and supplies the stream).
+include/wait_kv.h (the argument checks are in csrc/kv_binding.cpp; PyTorch
+allocates buffers and supplies the stream).
 
 * ``rotary_table`` / ``rotary``: vectors turned by their positions.
 * ``Cache``: one layer's paged cache, in 16 bits or quantised to 8.
@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import os
 import struct
 from typing import Optional
 
@@ -23,21 +24,19 @@ import torch
 from . import binding as B
 
 BF16, FP16, FP32, FP8, INT8 = 0, 1, 2, 3, 4
-_TYPE = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32,
-         torch.float8_e4m3fn: FP8, torch.int8: INT8}
-_WIDE = (torch.bfloat16, torch.float16, torch.float32)
 CACHE_TYPES = (torch.bfloat16, torch.float16, torch.float8_e4m3fn, torch.int8)
 EIGHT_BIT = (torch.float8_e4m3fn, torch.int8)
 
 
-# The structs of include/wait_kv.h, packed: a call's marshalling is most of a
-# small operator's time, and bytes cost a fraction of ctypes' structures.
+BINDING = os.path.join(B.PKG, "_kv.so")
+
+# The structs of include/wait_kv.h, for calls of the C ABI through ``_lib``.
 ROWS = struct.Struct("Pqqi4x")              # ws_kv_rows
 TURN = struct.Struct("PPiiii")              # ws_kv_turn
 CACHE = struct.Struct("PPPPiiiii4x")        # ws_kv_cache
 BATCH = struct.Struct("Pqi4xPPiiifiiii")    # ws_kv_batch
 
-_fn = None
+_fn = _kv = None
 
 
 def _lib():
@@ -54,81 +53,29 @@ def _lib():
     return _fn
 
 
-def _stream(index: int) -> int:
-    return torch.cuda.current_stream(index).cuda_stream
-
-
-# the same without building objects, where this PyTorch has them
-_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
-_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-
-
-def _run(fn, index: int, *args):
-    """fn(*args, the current stream) on GPU number `index`."""
-    if index < 0:
-        raise ValueError("the operators run on the GPU")
-    if _current() == index:
-        rc = fn(*args, _stream(index))
-    else:
-        with torch.cuda.device(index):
-            rc = fn(*args, _stream(index))
-    if rc:
-        B._check(rc)
+def _native():
+    """The checks and calls in C++ (csrc/kv_binding.cpp), bound to the library."""
+    global _kv
+    if _kv is None:
+        if not os.path.exists(BINDING):
+            raise RuntimeError(f"{BINDING} is missing: build it with paper_2504_11320_amd/build.py")
+        from . import _kv as native
+        L = _lib()
+        # streams and devices without building objects, where this PyTorch can
+        stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                         lambda i: torch.cuda.current_stream(i).cuda_stream)
+        current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        native.bind(*(C.cast(f, C.c_void_p).value for f in (
+            L.wait_kv_rotary, L.wait_kv_append, L.wait_kv_read,
+            L.wait_kv_attention_workspace_bytes, L.wait_kv_attention)),
+            B._check, stream, current, torch.cuda.device)
+        _kv = native
+    return _kv
 
 
 def _need(ok: bool, msg: str):
     if not ok:
         raise ValueError(msg)
-
-
-def _rows(t: torch.Tensor, name: str, index: int, types=_WIDE) -> bytes:
-    """The struct of t [tokens, heads, dim], on GPU number `index`."""
-    step = t.stride()
-    dtype = t.dtype
-    if len(step) != 3 or dtype not in types or step[2] != 1 or t.get_device() != index:
-        _need(len(step) == 3, f"{name} must be [tokens, heads, dim]")
-        _need(dtype in types, f"{name} must be one of {types}, is {dtype}")
-        _need(step[2] == 1 or t.shape[2] == 1, f"{name}: a vector's elements must be contiguous")
-        _need(t.get_device() == index, f"{name} must be on the same device, is on {t.device}")
-    return ROWS.pack(t.data_ptr(), step[0], step[1], _TYPE[dtype])
-
-
-def _fresh(t: torch.Tensor) -> bytes:
-    """The struct of a contiguous tensor made here."""
-    _, heads, dim = t.shape
-    return ROWS.pack(t.data_ptr(), heads * dim, dim, _TYPE[t.dtype])
-
-
-def _apart(t: torch.Tensor, name: str):
-    """Refuse an output whose rows share memory."""
-    need = t.shape[2]
-    for size, step in sorted(((t.shape[0], t.stride(0)), (t.shape[1], t.stride(1))),
-                             key=lambda x: abs(x[1])):
-        if size > 1:
-            _need(abs(step) >= need, f"{name}: rows must not overlap")
-            need = abs(step) * (size - 1) + need
-
-
-def _turn(positions, table, n: int, dim: int, interleaved: bool, index: int) -> bytes:
-    if positions is None or table is None:
-        raise ValueError("a rotation needs positions and a table")
-    size = table.shape
-    kind = positions.dtype
-    if (len(size) != 2 or table.dtype is not torch.float32 or not table.is_contiguous()
-            or positions.shape != (n,) or not positions.is_contiguous()
-            or (kind is not torch.int64 and kind is not torch.int32) or size[1] % 2
-            or not 2 <= size[1] <= dim or positions.get_device() != index
-            or table.get_device() != index):
-        _need(len(size) == 2 and table.dtype == torch.float32 and table.is_contiguous(),
-              "table must be [positions, part], fp32, contiguous")
-        _need(positions.shape == (n,) and positions.is_contiguous()
-              and kind in (torch.int64, torch.int32),
-              "positions must be one int64 or int32 a token, contiguous")
-        _need(size[1] % 2 == 0 and 2 <= size[1] <= dim,
-              "the table's part must be even, at least 2 and at most the head dimension")
-        raise ValueError("positions and table must be on the vectors' device")
-    return TURN.pack(table.data_ptr(), positions.data_ptr(), kind is torch.int32, size[0], size[1],
-                     bool(interleaved))
 
 
 # ----------------------------------------------------------------- rotary ----
@@ -182,22 +129,7 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *,
     (2 i, 2 i + 1) where ``interleaved``.  ``inverse`` turns back; that is the
     gradient's way through a rotation.  ``out`` may be x.  A position outside
     the table gives NaN."""
-    fn = _lib().wait_kv_rotary
-    index = x.get_device()
-    xr = _rows(x, "x", index)
-    n, heads, dim = x.shape
-    t = _turn(positions, table, n, dim, interleaved, index)
-    if out is None:
-        out = torch.empty_like(x)
-    else:
-        _need(out.shape == x.shape and out.dtype == x.dtype, "out must have x's shape and type")
-        _apart(out, "out")
-        _rows(out, "out", index)
-    if n and heads:
-        step = out.stride()
-        _run(fn, index, xr, ROWS.pack(out.data_ptr(), step[0], step[1], _TYPE[out.dtype]), n, heads,
-             dim, t, inverse)
-    return out
+    return _native().rotary(x, positions, table, interleaved, inverse, out)
 
 
 # ------------------------------------------------------------------ cache ----
@@ -212,28 +144,10 @@ class Cache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        size, dtype, index = k.shape, k.dtype, k.get_device()
-        if (len(size) != 4 or size != v.shape or dtype is not v.dtype or dtype not in CACHE_TYPES
-                or not k.is_contiguous() or not v.is_contiguous() or v.get_device() != index):
-            raise ValueError("k and v must both be [pages, kv_heads, page_size, dim] of one of "
-                             f"{CACHE_TYPES}, contiguous, on one device")
-        kp = vp = 0
-        if dtype in EIGHT_BIT:
-            _need(k_scale is not None and v_scale is not None, "an 8-bit cache needs scales")
-            rows = size[:3]
-            for t in (k_scale, v_scale):
-                if (t.shape != rows or t.dtype is not torch.float32 or not t.is_contiguous()
-                        or t.get_device() != index):
-                    raise ValueError("scales must be [pages, kv_heads, page_size], fp32, "
-                                     "contiguous, on the cache's device")
-            kp, vp = k_scale.data_ptr(), v_scale.data_ptr()
-        else:
-            _need(k_scale is None and v_scale is None, "a 16-bit cache has no scales")
+        self._c = _native().cache(k, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.pages, self.kv_heads, self.page_size, self.dim = size
-        self.dtype, self.device, self._index = dtype, k.device, index
-        self._c = CACHE.pack(k.data_ptr(), v.data_ptr(), kp, vp, self.pages, self.page_size,
-                             self.kv_heads, self.dim, _TYPE[dtype])
+        self.pages, self.kv_heads, self.page_size, self.dim = k.shape
+        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
 
     @classmethod
     def empty(cls, pages: int, page_size: int, kv_heads: int, dim: int,
@@ -250,14 +164,6 @@ class Cache:
         return 2 * kv_heads * (dim * dtype.itemsize + (4 if dtype in EIGHT_BIT else 0))
 
 
-def _slots(slots: torch.Tensor, index: int) -> int:
-    size = slots.shape
-    _need(len(size) == 1 and slots.dtype is torch.int64 and slots.is_contiguous()
-          and slots.get_device() == index,
-          "slots must be one int64 a token, contiguous, on the cache's device")
-    return size[0]
-
-
 def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *,
            positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
            interleaved: bool = False) -> None:
@@ -266,40 +172,15 @@ def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
     negative, or behind the cache's end, is left out.  With ``positions`` and
     ``table`` the keys are turned first, as by ``rotary``, without a rounding
     between."""
-    fn = _lib().wait_kv_append
-    index = cache._index
-    kr, vr = _rows(k, "k", index), _rows(v, "v", index)
-    n = _slots(slots, index)
-    _need(k.shape == (n, cache.kv_heads, cache.dim) and k.shape == v.shape and k.dtype is v.dtype,
-          "k and v must be [slots, kv_heads, dim] of one type")
-    t = None
-    if positions is not None or table is not None:
-        t = _turn(positions, table, n, cache.dim, interleaved, index)
-    _run(fn, index, cache._c, kr, vr, slots.data_ptr(), n, t)
+    _native().append(cache._c, cache._index, k, v, slots, positions, table, interleaved)
 
 
 def read(cache: Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
          out: Optional[tuple] = None) -> tuple:
     """(k, v) [slots, kv_heads, dim] of the cache's slots, as values rounded
     once to ``dtype``; zeros for a slot that the cache does not have."""
-    fn = _lib().wait_kv_read
-    index = cache._index
-    n = _slots(slots, index)
-    shape = (n, cache.kv_heads, cache.dim)
-    if out is None:
-        _need(dtype in _WIDE, f"dtype must be one of {_WIDE}")
-        k = torch.empty(*shape, dtype=dtype, device=cache.device)
-        v = torch.empty_like(k)
-        kr, vr = _fresh(k), _fresh(v)
-    else:
-        k, v = out
-        _need(k.shape == shape and v.shape == shape and k.dtype is v.dtype,
-              "out must be two [slots, kv_heads, dim] of one type")
-        _apart(k, "k")
-        _apart(v, "v")
-        kr, vr = _rows(k, "k", index), _rows(v, "v", index)
-    _run(fn, index, cache._c, slots.data_ptr(), n, kr, vr)
-    return k, v
+    a, b = (None, None) if out is None else out
+    return _native().read(cache._c, cache._index, slots, dtype, a, b)
 
 
 # -------------------------------------------------------------- attention ----
@@ -325,62 +206,8 @@ def attention(q: torch.Tensor, cache: Cache, pages: torch.Tensor, starts: torch.
     Returns out, or (out, lse [tokens, heads] fp32).  ``workspace`` (a uint8
     tensor of ``attention_workspace_bytes``) is taken from PyTorch where it is
     not given."""
-    L = _lib()
-    index = cache._index
-    qr = _rows(q, "q", index, _WIDE[:2])
-    size = q.shape
-    _need(size[2] == cache.dim, "q and the cache must have one head dimension")
-    _need(cache.dtype in EIGHT_BIT or q.dtype is cache.dtype,
-          "q must have the type of a 16-bit cache")
-    batch, need = _batch(size, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, causal,
-                         window)
-    if out is None:
-        out = torch.empty_like(q)
-    else:
-        _need(out.shape == size and out.dtype is q.dtype, "out must have q's shape and type")
-        _apart(out, "out")
-    lse = torch.empty(size[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    ptr, have = None, 0
-    if workspace is not None:
-        _need(workspace.is_contiguous() and workspace.get_device() == index,
-              "workspace must be contiguous, on the cache's device")
-        ptr, have = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    elif need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        ptr, have = workspace.data_ptr(), need
-    _run(L.wait_kv_attention, index, cache._c, batch, qr, _rows(out, "out", index),
-         None if lse is None else lse.data_ptr(), ptr, have)
-    return out if lse is None else (out, lse)
-
-
-def _batch(size, cache, pages, starts, kv_lens, max_q_len, max_kv_len, scale, causal, window):
-    """(the struct of a batch, the bytes of its workspace)."""
-    index = cache._index
-    T, heads, dim = size
-    n_seq, cols = pages.shape if pages.dim() == 2 else (-1, 0)
-    step = pages.stride()
-    if (n_seq < 0 or pages.dtype is not torch.int32 or (step[1] != 1 and cols > 1)
-            or pages.get_device() != index):
-        raise ValueError("pages must be [requests, pages], int32, rows contiguous, on the cache's "
-                         "device")
-    for t, n in ((starts, n_seq + 1), (kv_lens, n_seq)):
-        if (t.shape != (n,) or t.dtype is not torch.int32 or not t.is_contiguous()
-                or t.get_device() != index):
-            raise ValueError("starts (one more than the requests) and kv_lens (one each) must be "
-                             "int32, contiguous, on the cache's device")
-    _need(heads >= 1 and heads % cache.kv_heads == 0, "heads must be a multiple of the cache's")
-    cap = cols * cache.page_size
-    b = BATCH.pack(pages.data_ptr(), step[0] if n_seq > 1 else cols, cols, starts.data_ptr(),
-                   kv_lens.data_ptr(), n_seq, T, heads,
-                   1.0 / math.sqrt(dim) if scale is None else scale, bool(causal),
-                   min(window, 0x7fffffff),
-                   T if max_q_len is None else min(max_q_len, T),
-                   cap if max_kv_len is None else min(max_kv_len, cap))
-    need = C.c_size_t()
-    rc = _lib().wait_kv_attention_workspace_bytes(cache._c, b, need)
-    if rc:
-        B._check(rc)
-    return b, need.value
+    return _native().attention(cache._c, cache._index, q, pages, starts, kv_lens, max_q_len,
+                               max_kv_len, scale, causal, window, return_lse, out, workspace)
 
 
 def attention_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor,
@@ -388,5 +215,5 @@ def attention_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor
                               max_q_len: Optional[int] = None, max_kv_len: Optional[int] = None,
                               window: int = 0) -> int:
     """Bytes that ``attention`` takes as its workspace for these shapes."""
-    return _batch(q.shape, cache, pages, starts, kv_lens, max_q_len, max_kv_len, None, True,
-                  window)[1]
+    return _native().attention_workspace_bytes(cache._c, cache._index, q, pages, starts, kv_lens,
+                                               max_q_len, max_kv_len, window)
