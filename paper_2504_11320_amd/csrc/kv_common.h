@@ -132,7 +132,7 @@ struct Fp32 {
 // N elements of type T at p, in as few accesses as VEC allows (VEC elements
 // each; the caller vouches for their alignment).
 template <class T, int N, int VEC>
-__device__ __forceinline__ void load_n(const typename T::raw *p, float (&x)[N]) {
+__device__ __forceinline__ void load_raw(const typename T::raw *p, typename T::raw (&x)[N]) {
   struct alignas(VEC * sizeof(typename T::raw)) Pack {
     typename T::raw r[VEC];
   };
@@ -140,8 +140,15 @@ __device__ __forceinline__ void load_n(const typename T::raw *p, float (&x)[N]) 
   for (int i = 0; i < N; i += VEC) {
     Pack v = *reinterpret_cast<const Pack *>(p + i);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) x[i + j] = T::get(v.r[j]);
+    for (int j = 0; j < VEC; ++j) x[i + j] = v.r[j];
   }
+}
+template <class T, int N, int VEC>
+__device__ __forceinline__ void load_n(const typename T::raw *p, float (&x)[N]) {
+  typename T::raw r[N];
+  load_raw<T, N, VEC>(p, r);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = T::get(r[i]);
 }
 // STREAM: past the caches, for outputs that these cannot hold.
 template <class T, int N, int VEC, bool STREAM = false>

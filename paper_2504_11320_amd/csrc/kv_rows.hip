@@ -14,11 +14,24 @@ struct TurnArgs {
   int32_t positions_32, n_table, part;
 };
 
-// The table's row of token i, or NULL where its position has none.
-__device__ __forceinline__ const float *turn_row(const TurnArgs &t, int64_t i) {
-  int64_t p = t.positions_32 ? (int64_t)((const int32_t *)t.positions)[i]
-                             : ((const int64_t *)t.positions)[i];
-  return p >= 0 && p < t.n_table ? t.table + p * t.part : nullptr;
+// A token's position as its two words (of 32 bits: twice the only one), asked for
+// and not yet waited for.
+struct Position {
+  uint32_t lo, hi;
+};
+__device__ __forceinline__ Position ask_position(const TurnArgs &t, int64_t i) {
+  const uint32_t *p = (const uint32_t *)t.positions + (t.positions_32 ? i : 2 * i);
+  return {p[0], p[t.positions_32 ? 0 : 1]};
+}
+// Nothing is asked for later than this that is written before it, and the
+// position is used behind it only.
+__device__ __forceinline__ void all_asked(Position &p) {
+  asm volatile("" : "+v"(p.lo), "+v"(p.hi) : : "memory");
+}
+// The table's row of a position, or NULL where it has none.
+__device__ __forceinline__ const float *turn_row(const TurnArgs &t, Position p) {
+  const bool is = p.lo < (uint32_t)t.n_table && (t.positions_32 || p.hi == 0);
+  return is ? t.table + (int64_t)p.lo * t.part : nullptr;
 }
 
 // ------------------------------------------------------------ rotary -----
@@ -36,8 +49,8 @@ struct RotaryArgs {
 };
 
 // Outputs from this size on are larger than the second level caches together,
-// and are written past them.  8192 x 32 vectors of 128 bf16 elements (67 MB each
-// way): 23.5 us against 30.0.
+// and are written past them, which took a fifth off the time of 8192 x 32 vectors
+// of 128 bf16 elements (67 MB each way): 21.5 us.
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 
 // A thread takes one work item of HPT heads of a token: VEC elements and their
@@ -60,17 +73,20 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
   const bool copy = item >= a.turned;
   const int32_t d = copy ? part + (item - a.turned) * VEC : item * VEC;
   constexpr int NC = INTER ? (VEC + 1) / 2 : VEC;
-  // the vectors are asked for before the angles, which wait for the position
-  float u[HPT][VEC], w[HPT][VEC];
+  // the position first, which the angles wait for, then the vectors; a value is
+  // used only behind the last request, because using it is waiting for it
+  Position position = ask_position(a.turn, token);
+  raw u0[HPT][VEC], w0[HPT][VEC];
 #pragma unroll
   for (int k = 0; k < HPT; ++k) {
     const int32_t h = min(h0 + k, a.heads - 1);
-    load_n<T, VEC, VEC>(x + h * a.xh + d, u[k]);
-    if (!INTER && !copy) load_n<T, VEC, VEC>(x + h * a.xh + half + d, w[k]);
+    load_raw<T, VEC, VEC>(x + h * a.xh + d, u0[k]);
+    if constexpr (!INTER) load_raw<T, VEC, VEC>(x + h * a.xh + (copy ? d : half + d), w0[k]);
   }
+  all_asked(position);
   float c[NC], s[NC];
   if (!copy) {
-    const float *row = turn_row(a.turn, token);
+    const float *row = turn_row(a.turn, position);
     const int32_t i0 = INTER ? d / 2 : d;
     if (row) {
 #pragma unroll
@@ -88,22 +104,26 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
     const int32_t h = h0 + k;
     if (h >= a.heads) continue;
     raw *o = out + h * a.oh + d;
+    float u[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) u[i] = T::get(u0[k][i]);
     if (copy) {
-      store_n<T, VEC, VEC, STREAM>(o, u[k]);
+      store_n<T, VEC, VEC, STREAM>(o, u);
     } else if constexpr (INTER) {
       float y[VEC];
 #pragma unroll
       for (int i = 0; i < VEC / 2; ++i) {
-        y[2 * i] = u[k][2 * i] * c[i] - u[k][2 * i + 1] * s[i];
-        y[2 * i + 1] = u[k][2 * i + 1] * c[i] + u[k][2 * i] * s[i];
+        y[2 * i] = u[2 * i] * c[i] - u[2 * i + 1] * s[i];
+        y[2 * i + 1] = u[2 * i + 1] * c[i] + u[2 * i] * s[i];
       }
       store_n<T, VEC, VEC, STREAM>(o, y);
     } else {
       float y[VEC], z[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        y[i] = u[k][i] * c[i] - w[k][i] * s[i];
-        z[i] = w[k][i] * c[i] + u[k][i] * s[i];
+        const float w = T::get(w0[k][i]);
+        y[i] = u[i] * c[i] - w * s[i];
+        z[i] = w * c[i] + u[i] * s[i];
       }
       store_n<T, VEC, VEC, STREAM>(o, y);
       store_n<T, VEC, VEC, STREAM>(o + half, z);
@@ -174,7 +194,7 @@ __global__ void __launch_bounds__(256) rotary_single_kernel(RotaryArgs a) {
     out[part + item - half] = x[part + item - half];
     return;
   }
-  const float *row = turn_row(a.turn, token);
+  const float *row = turn_row(a.turn, ask_position(a.turn, token));
   const float c = row ? row[item] : NAN;
   float s = row ? row[half + item] : NAN;
   if (a.inverse) s = -s;
@@ -208,15 +228,23 @@ struct AppendArgs {
   const int64_t *slots;
   int64_t n, n_slots;
   int32_t heads, page_shift;
+  int32_t head_groups;  // groups of H heads
   int32_t interleaved;
   TurnArgs turn;
 };
 
+// Beyond the threads that the card holds at once, a thread takes two heads.
+// 8191 x 8 rows of 128, fp16 into int8: 12.5 us against 13.6 with one head a
+// thread, 14.0 with four, 16.7 with eight; 1024 x 32 rows, bf16 into fp8, which it
+// holds: 8.6 against 7.9.
+constexpr int kHeads = 2;
+constexpr int64_t kResidentThreads = 256 * 2048;
+
 // A row's eight elements u, d .. d+7, of this lane turned by the angles of
-// `row`.  Where the halves are multiples of eight, w holds their partners.
+// `row`, element by element: neighbours, or halves that do not fill lanes.
 template <class T>
-__device__ __forceinline__ void turn_lane(const typename T::raw *x, int d, const AppendArgs &a,
-                                          const float *row, const float (&w)[8], float (&u)[8]) {
+__device__ __forceinline__ void turn_any(const typename T::raw *x, int d, const AppendArgs &a,
+                                         const float *row, float (&u)[8]) {
   const int part = a.turn.part, half = part / 2;
   if (d >= part) return;
   if (a.interleaved) {
@@ -227,21 +255,6 @@ __device__ __forceinline__ void turn_lane(const typename T::raw *x, int d, const
       const float p = u[i], q = u[i + 1];
       u[i] = p * c - q * s;
       u[i + 1] = q * c + p * s;
-    }
-    return;
-  }
-  if (half % 8 == 0) {
-    const bool low = d < half;
-    const int i0 = low ? d : d - half;
-    if (!row) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = NAN;
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float c = row[i0 + i], s = row[half + i0 + i];
-      u[i] = low ? u[i] * c - w[i] * s : u[i] * c + w[i] * s;
     }
     return;
   }
@@ -277,7 +290,7 @@ __device__ __forceinline__ void put_row(void *base, float *scales, int64_t row, 
     if (some) {
       float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(u[i] * by, -most), most);
+      for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_fmed3f(u[i] * by, -most, most);
       if constexpr (TYPE == WS_KV_FP8) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -285,9 +298,16 @@ __device__ __forceinline__ void put_row(void *base, float *scales, int64_t row, 
           code[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], w, true);
         }
       } else {
+        // at 1.5 * 2^23 the last place of a float is 1: the low byte is the code
+        uint32_t n[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          code[i / 4] |= ((uint32_t)(int)rintf(y[i]) & 0xffu) << (8 * (i % 4));
+        for (int i = 0; i < 8; ++i) n[i] = __float_as_uint(y[i] + 12582912.0f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t lo = __builtin_amdgcn_perm(n[4 * i + 1], n[4 * i], 0x0c0c0400u);
+          const uint32_t hi = __builtin_amdgcn_perm(n[4 * i + 3], n[4 * i + 2], 0x04000c0cu);
+          code[i] = lo | hi;
+        }
       }
     }
     *reinterpret_cast<u32x2 *>((uint8_t *)base + row * dim + lane * 8) = code;
@@ -295,48 +315,97 @@ __device__ __forceinline__ void put_row(void *base, float *scales, int64_t row, 
   }
 }
 
-// G = dim / 8 lanes take the two rows of a (token, head), which are read and
-// written once, whole lines each.  8191 x 8 rows of 128, fp16 into int8, the keys
-// turned (50 MB): 17.6 us (2.9 TB/s), bound by the waits of slots, angles and rows.
-template <class T, int TYPE, int G, int VEC>
+// G = dim / 8 lanes take the two rows of H heads of a token, which are read and
+// written once, whole lines each; slot, position and angles are read once for
+// the H.  LANES: nothing is turned, or halves of whole lanes.
+// 8191 x 8 rows of 128, fp16 into int8, the keys turned (50 MB): 12.5 us (4.0
+// TB/s), 17.1 with a wait at each request for what is converted there.
+template <class T, int TYPE, int G, int VEC, int H, bool LANES>
 __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   using raw = typename T::raw;
   constexpr int dim = 8 * G;
   const int lane = threadIdx.x % G;
   const uint32_t id = blockIdx.x * (256u / G) + threadIdx.x / G;
-  const int64_t token = id / (uint32_t)a.heads;
-  const int32_t h = (int32_t)(id % (uint32_t)a.heads);
+  const int64_t token = id / (uint32_t)a.head_groups;
+  const int32_t h0 = (int32_t)(id - (uint32_t)token * (uint32_t)a.head_groups) * H;
   if (token >= a.n) return;  // the G lanes of a row end together
-  const raw *k = (const raw *)a.k + token * a.kt + h * a.kh;
-  const raw *v = (const raw *)a.v + token * a.vt + h * a.vh;
+  const raw *k = (const raw *)a.k + token * a.kt;
+  const raw *v = (const raw *)a.v + token * a.vt;
   const int d = lane * 8;
-  // everything is asked for before the slot says whether it is wanted; partners
-  // in a rotation come by a second read, which the first level cache answers
-  float x[8], y[8], w[8] = {};
-  load_n<T, 8, VEC>(k + d, x);
-  load_n<T, 8, VEC>(v + d, y);
+  // Everything is asked for before the first use of any of it, the position
+  // first, which the angles wait for; partners in a rotation come by a second
+  // read, which the first level cache answers.
   const bool turn = a.turn.positions != nullptr;
   const int half = a.turn.part / 2;
-  if (turn && !a.interleaved && half % 8 == 0 && d < a.turn.part)
-    load_n<T, 8, VEC>(k + (d < half ? d + half : d - half), w);
-  const float *angles = turn ? turn_row(a.turn, token) : nullptr;
+  const bool low = d < half, turned = LANES && turn && d < a.turn.part;
+  const int partner = !turned ? d : low ? d + half : d - half;
+  Position position = {};
+  if (turn) position = ask_position(a.turn, token);
   const int64_t slot = a.slots[token];
+  raw x[H][8], y[H][8], w[H][8];
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int32_t h = min(h0 + i, a.heads - 1);
+    load_raw<T, 8, VEC>(k + h * a.kh + d, x[i]);
+    load_raw<T, 8, VEC>(v + h * a.vh + d, y[i]);
+    if constexpr (LANES) load_raw<T, 8, VEC>(k + h * a.kh + partner, w[i]);
+  }
+  all_asked(position);
+  const float *angles = turn ? turn_row(a.turn, position) : nullptr;
+  float c[8], s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c[e] = s[e] = NAN;
+  if (turned && angles) {
+    const float *p = angles + (low ? d : d - half);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      c[e] = p[e];
+      s[e] = p[half + e];
+    }
+  }
   if (slot < 0 || slot >= a.n_slots) return;
-  if (turn) turn_lane<T>(k, d, a, angles, w, x);
   const int64_t page = slot >> a.page_shift, off = slot & ((1 << a.page_shift) - 1);
-  const int64_t row = ((page * a.heads + h) << a.page_shift) + off;
-  put_row<TYPE, G>(a.ck, a.ks, row, lane, dim, x);
-  put_row<TYPE, G>(a.cv, a.vs, row, lane, dim, y);
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int32_t h = h0 + i;
+    if (h >= a.heads) break;
+    const int64_t row = ((page * a.heads + h) << a.page_shift) + off;
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = T::get(x[i][e]);
+    if constexpr (LANES) {
+      if (turned) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float other = T::get(w[i][e]);
+          u[e] = u[e] * c[e] + (low ? -other : other) * s[e];
+        }
+      }
+    } else if (turn) {
+      turn_any<T>(k + h * a.kh, d, a, angles, u);
+    }
+    put_row<TYPE, G>(a.ck, a.ks, row, lane, dim, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = T::get(y[i][e]);
+    put_row<TYPE, G>(a.cv, a.vs, row, lane, dim, u);
+  }
 }
 
 template <class T, int TYPE, int G>
-int append_launch(const AppendArgs &a, int vec, hipStream_t stream) {
-  const int64_t blocks = (a.n * a.heads + 256 / G - 1) / (256 / G);
+int append_launch(AppendArgs a, int vec, hipStream_t stream) {
   constexpr int wide = 16 / sizeof(typename T::raw);
-  if (vec >= wide)
-    append_kernel<T, TYPE, G, wide><<<dim3((uint32_t)blocks), 256, 0, stream>>>(a);
+  const bool lanes = vec >= wide && !a.interleaved && a.turn.part % 16 == 0;
+  const bool many = lanes && a.heads >= kHeads && a.n * a.heads * G > kResidentThreads;
+  a.head_groups = many ? (a.heads + kHeads - 1) / kHeads : a.heads;
+  const dim3 blocks((uint32_t)((a.n * a.head_groups + 256 / G - 1) / (256 / G)));
+  if (many)
+    append_kernel<T, TYPE, G, wide, kHeads, true><<<blocks, 256, 0, stream>>>(a);
+  else if (lanes)
+    append_kernel<T, TYPE, G, wide, 1, true><<<blocks, 256, 0, stream>>>(a);
+  else if (vec >= wide)
+    append_kernel<T, TYPE, G, wide, 1, false><<<blocks, 256, 0, stream>>>(a);
   else
-    append_kernel<T, TYPE, G, 1><<<dim3((uint32_t)blocks), 256, 0, stream>>>(a);
+    append_kernel<T, TYPE, G, 1, 1, false><<<blocks, 256, 0, stream>>>(a);
   return launched();
 }
 
