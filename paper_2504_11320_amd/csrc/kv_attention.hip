@@ -1125,58 +1125,65 @@ __global__ void __launch_bounds__(64 * kWideWaves<D>, D == 256 ? 1 : 2) rows_ker
 
 // ----------------------------------------------------------- joining ----
 //
-// A wave joins parts of a (token, head), D / 64 elements a lane.
+// D / 4 lanes join parts of a (token, head), four elements each.
 
 template <int D>
+constexpr int kJoinLanes = D / 4;
+
 struct Joined {
-  float o[D / 64];
+  f32x4 o;
   float m, l;
 };
 
+__device__ __forceinline__ void join(Joined &j, f32x4 o, float m, float l) {
+  const float top = fmaxf(j.m, m), base = top == -INFINITY ? 0.0f : top;
+  const float ej = exp2_of(j.m - base), e = exp2_of(m - base);
+  j.m = top;
+  j.l = j.l * ej + l * e;
+  j.o = j.o * ej + o * e;
+}
+
+// The parts first, first + step, ...: four at a time are under way.
 template <int D>
-__device__ __forceinline__ Joined<D> join_parts(const float *part_o, const float2 *part_ml,
-                                                int32_t first, int32_t step, int32_t parts) {
-  constexpr int per = D / 64;
-  const int lane = threadIdx.x & 63;
-  Joined<D> j;
-  j.m = -INFINITY;
-  for (int32_t k = first + step * lane; k < parts; k += 64 * step) j.m = fmaxf(j.m, part_ml[k].x);
+__device__ __forceinline__ Joined join_parts(const float *part_o, const float2 *part_ml,
+                                             int32_t first, int32_t step, int32_t parts) {
+  constexpr int ahead = 4;
+  const int lane = threadIdx.x % kJoinLanes<D>;
+  Joined j = {f32x4{0, 0, 0, 0}, -INFINITY, 0.0f};
+  for (int32_t k = first; k < parts; k += ahead * step) {
+    f32x4 o[ahead];
+    float2 ml[ahead];
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) j.m = fmaxf(j.m, __shfl_xor(j.m, x));
-  const float base = j.m == -INFINITY ? 0.0f : j.m;
-  j.l = 0.0f;
+    for (int i = 0; i < ahead; ++i) {
+      const int64_t at = min(k + i * step, parts - 1);
+      ml[i] = part_ml[at];
+      o[i] = *reinterpret_cast<const f32x4 *>(part_o + at * D + 4 * lane);
+    }
 #pragma unroll
-  for (int i = 0; i < per; ++i) j.o[i] = 0.0f;
-#pragma unroll 4
-  for (int32_t k = first; k < parts; k += step) {
-    const float2 ml = part_ml[k];
-    const float e = exp2_of(ml.x - base);
-    j.l += ml.y * e;
-#pragma unroll
-    for (int i = 0; i < per; ++i) j.o[i] += part_o[(int64_t)k * D + lane * per + i] * e;
+    for (int i = 0; i < ahead; ++i)
+      if (k + i * step < parts) join(j, o[i], ml[i].x, ml[i].y);
   }
   return j;
 }
 
 template <int D>
-__device__ __forceinline__ void put_joined(const Args &a, const Joined<D> &j, int64_t q_row,
+__device__ __forceinline__ void put_joined(const Args &a, const Joined &j, int64_t q_row,
                                            int32_t head) {
-  constexpr int per = D / 64;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x % kJoinLanes<D>;
   const float inv = safe_inverse(j.l);
-  uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + lane * per;
+  uint16_t *p = a.out + q_row * a.ot + (int64_t)head * a.oh + 4 * lane;
 #pragma unroll
-  for (int i = 0; i < per; ++i) p[i] = out_bits(a, j.o[i] * inv);
+  for (int i = 0; i < 4; ++i) p[i] = out_bits(a, j.o[i] * inv);
   if (a.lse && lane == 0) a.lse[q_row * a.heads + head] = natural_lse(j.m, j.l);
 }
 
-// Few rows have many parts: four waves share a (request, head), of which they
-// take the tokens `nth`, `nth` + `step`, ...
+// Few rows have many parts: a workgroup shares a (request, head), of which it
+// takes the tokens `nth`, `nth` + `step`, ...
 template <int D>
 __device__ __forceinline__ void join_few(const Args &a, int32_t id, int32_t nth, int32_t step) {
-  constexpr int per = D / 64;
-  __shared__ Joined<D> shared[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int lanes = kJoinLanes<D>, groups = 256 / lanes;
+  __shared__ Joined shared[groups][lanes];
+  const int lane = threadIdx.x % lanes, mine = threadIdx.x / lanes;
   const int32_t head = id % a.heads, b = id / a.heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
@@ -1188,19 +1195,14 @@ __device__ __forceinline__ void join_few(const Args &a, int32_t id, int32_t nth,
         few_parts(a, block_range(a, s, r0, min(r0 + kFewRows, rows) - 1, 32), rows);
     if (parts == 1) continue;
     const int64_t at = (from + row) * a.few_splits;
-    shared[wave][lane] = join_parts<D>(a.few_o + at * D, a.few_ml + at, wave, 4, parts);
+    shared[mine][lane] = join_parts<D>(a.few_o + at * D, a.few_ml + at, mine, groups, parts);
     __syncthreads();
-    if (wave == 0) {
-      Joined<D> j = shared[0][lane];
+    if (mine == 0) {
+      Joined j = shared[0][lane];
 #pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        const Joined<D> x = shared[w][lane];
-        const float top = fmaxf(j.m, x.m), base = top == -INFINITY ? 0.0f : top;
-        const float ej = exp2_of(j.m - base), ex = exp2_of(x.m - base);
-        j.m = top;
-        j.l = j.l * ej + x.l * ex;
-#pragma unroll
-        for (int k = 0; k < per; ++k) j.o[k] = j.o[k] * ej + x.o[k] * ex;
+      for (int g = 1; g < groups; ++g) {
+        const Joined x = shared[g][lane];
+        join(j, x.o, x.m, x.l);
       }
       put_joined<D>(a, j, s.q0 + i, head);
     }
@@ -1208,15 +1210,16 @@ __device__ __forceinline__ void join_few(const Args &a, int32_t id, int32_t nth,
   }
 }
 
-// Many rows have few parts: a wave to a (token, head).  (Four heads a wave, with
-// their loads under way together, took 53 us instead of 31 where 200 x 8 rows have
-// 16 parts, and saved nothing where 543 x 32 have 3.)
+// Many rows have few parts: a wave to 64 / kJoinLanes heads of a token.
 template <int D>
 __device__ __forceinline__ void join_many(const Args &a, int32_t id, int32_t keys) {
-  const int32_t head = id % a.heads, token = id / a.heads;
+  constexpr int several = 64 / kJoinLanes<D>;
+  const int32_t head_groups = (a.heads + several - 1) / several;
+  const int32_t token = id / head_groups;
   if (token >= a.n_tokens) return;
+  const int32_t head = id % head_groups * several + (threadIdx.x & 63) / kJoinLanes<D>;
   const int32_t b = last_at_most(a, [&](int32_t i) { return a.starts[i] <= token; });
-  if (b < 0) return;
+  if (b < 0 || head >= a.heads) return;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group, i = token - s.q0;
   if (i < 0 || i >= s.n || rows <= kFewRows) return;
@@ -1229,7 +1232,7 @@ __device__ __forceinline__ void join_many(const Args &a, int32_t id, int32_t key
 }
 
 // Both in one launch: 64 heads with 32 parts each 4.8 us; 543 x 32 rows, most of
-// them with 3, 12 us.
+// them with 3, 7.2 us (12 with a wave a row, whose waves come in two turns).
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(Args a, int32_t few, int32_t step, int32_t keys) {
   if ((int32_t)blockIdx.x < few)
@@ -1346,7 +1349,8 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
     // a request whose few rows have parts has at most so many tokens
     const int32_t step = std::max(1, L.few_blocks * kFewRows / a.group);
     const int64_t few = L.few_slots ? (int64_t)a.n_seq * a.heads * step : 0;
-    const int64_t waves = (int64_t)a.n_tokens * a.heads;
+    constexpr int several = 64 / kJoinLanes<D>;
+    const int64_t waves = (int64_t)a.n_tokens * ceil_div(a.heads, several);
     const int64_t blocks = few + (L.many_slots ? ceil_div(waves, 4) : 0);
     if (blocks >= (int64_t)1 << 31)
       return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
