@@ -848,8 +848,10 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
       }
       if (keys && wave == 0 && lane < M::keys) {
         const bool next_edge = k1 < block_every.lo || k1 + M::keys > block_every.hi;
-        if (next_edge && !isfinite(vs)) {
-          bad |= key_there >> lane & 1;
+        if (!(key_there >> lane & 1)) {  // loaded from another row
+          ks = vs = 0.0f;
+        } else if (next_edge && !isfinite(vs)) {
+          bad = true;
           vs = 0.0f;
         }
         float *sc = (float *)(smem + 4 * M::side + ((t + 1) & 1) * M::scales);

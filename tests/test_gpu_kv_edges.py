@@ -1,0 +1,53 @@
+"""Attention and rows at the edges: pages that are not there beside scales and
+codes that are not finite, windows of any size, scales of either sign, contexts
+whose values are all zero, many requests."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_kv_attention import check, make
+
+pytestmark = pytest.mark.gpu
+
+BF, FP, F32 = torch.bfloat16, torch.float16, torch.float32
+E4, I8 = torch.float8_e4m3fn, torch.int8
+
+
+@pytest.fixture(scope="module")
+def kv():
+    from paper_2504_11320_amd import kv
+    return kv
+
+
+def free_page_zero(s):
+    """No request's page is page 0."""
+    c, p = s["cache"], s["pages"]
+    used = set(p[p >= 0].tolist())
+    if 0 in used:
+        other = min(set(range(c.pages)) - used)
+        for t in (c.k, c.v, c.k_scale, c.v_scale):
+            if t is not None:
+                raw = t.view(torch.uint8)
+                raw[other] = raw[0]
+        p[p == 0] = other
+
+
+@pytest.mark.parametrize("ctype", [E4, I8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_scales_of_keys_that_are_not_there(kv, ctype, dim, value):
+    """A page that a request lacks, among keys that all of its tokens see: no
+    other row of the cache takes part in its place, whatever scale that has."""
+    s = make(kv, [1, 100, 40], [100, 700, 300], 4, 2, dim, 16, ctype, BF)
+    free_page_zero(s)
+    c, p = s["cache"], s["pages"]
+    p[0, 2] = -1
+    p[1, 9], p[1, 20] = -1, c.pages
+    p[2, 3] = 1 << 30
+    c.k_scale[0], c.v_scale[0] = value, value
+    check(kv, s, f"hole beside a scale of {value}")
+    check(kv, s, f"hole beside a scale of {value}, no causal", causal=False)
+    check(kv, s, f"hole beside a scale of {value}, few rows", max_q_len=1)
+
+
