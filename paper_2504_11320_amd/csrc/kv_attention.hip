@@ -838,7 +838,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
         u32x4 x = reg[i];
         if (v && (edge || value_there != ~0ull)) {
           if (!(value_there >> key & 1)) x = u32x4{0, 0, 0, 0};
-          if (TYPE == WS_KV_FP8) bad |= take_nan_codes(x);
+          if (TYPE == WS_KV_FP8 && edge) bad |= take_nan_codes(x);
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {

@@ -51,3 +51,22 @@ def test_scales_of_keys_that_are_not_there(kv, ctype, dim, value):
     check(kv, s, f"hole beside a scale of {value}, few rows", max_q_len=1)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("hints", [{}, dict(max_q_len=1)])
+def test_nan_codes_beside_a_hole(kv, dim, hints):
+    """An fp8 code that is NaN reaches every token that sees it, where a page
+    beside it is not there as well."""
+    s = make(kv, [1, 100], [100, 700], 4, 2, dim, 16, E4, BF)
+    p = s["pages"]
+    p[0, 3], p[1, 9] = -1, -1
+    args = s["q"], s["cache"], p, s["starts"], s["kv_lens"]
+    want = kv.attention(*args, **hints)
+    assert bool(torch.isfinite(want).all())
+    for b, j in ((0, 40), (1, 135)):
+        s["cache"].v.view(torch.uint8)[int(p[b, j // 16]), 0, j % 16, 5] = 0x7F
+    got = kv.attention(*args, **hints)
+    assert bool(torch.isnan(got[:, :2, 5]).all())
+    got[:, :2, 5] = want[:, :2, 5]
+    assert torch.equal(got, want)
+
+
