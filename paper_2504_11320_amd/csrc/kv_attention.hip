@@ -88,7 +88,7 @@ __device__ __forceinline__ Range token_range(const Args &a, const Seq &s, int32_
   const int32_t p = s.m - s.n + i;
   r.hi = min(s.m, a.capacity);
   if (a.causal) r.hi = max(min(r.hi, p + 1), 0);
-  r.lo = a.window ? max(p - a.window + 1, 0) : 0;
+  r.lo = a.window && p >= a.window ? p - a.window + 1 : 0;  // p may be negative
   r.lo = min(r.lo, r.hi);
   return r;
 }

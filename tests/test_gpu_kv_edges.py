@@ -70,3 +70,20 @@ def test_nan_codes_beside_a_hole(kv, dim, hints):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("q,m", [([6, 1], [2, 3]), ([90, 5], [30, 1]), ([6, 1], [1500, 3])])
+def test_windows_without_end(kv, q, m, causal):
+    """A window larger than any request is none, for queries before the first
+    key too."""
+    s = make(kv, q, m, 2, 1, 64, 16, BF, BF)
+    args = s["q"], s["cache"], s["pages"], s["starts"], s["kv_lens"]
+    want, lse = kv.attention(*args, causal=causal, return_lse=True)
+    for window in (1 << 20, 2**31 - 100, 2**31 - 2, 2**31 - 1, 1 << 40):
+        got, other = kv.attention(*args, causal=causal, window=window, return_lse=True)
+        # the parts of a request may differ with the window: the same keys
+        check(kv, s, f"window {window}", causal, min(window, 1 << 40))
+        assert torch.equal(torch.isinf(other), torch.isinf(lse)), window
+        if max(m) < 100:
+            assert torch.equal(got, want) and torch.equal(other, lse), window
+
+
