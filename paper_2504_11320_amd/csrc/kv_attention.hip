@@ -245,6 +245,12 @@ __device__ __forceinline__ float unbounded_value(const Args &a, int32_t row, int
   return isfinite(x) ? 0.0f : x;
 }
 
+// Below this the reference of the softmax no longer follows a value's scale, the
+// weight still does: with the smallest scale of a stored row, 2^-100 / 448, it is
+// 2^-13, a normal number in 16 bits.  Where all values seen have smaller scales
+// (zeros), each key adds up to 2^96 to l, and 2^30 of them stay finite.
+constexpr float kLeastLog = -96.0f;
+
 // o / l in the output's type; a query that sees nothing has l = 0.
 __device__ __forceinline__ float safe_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ uint16_t out_bits(const Args &a, float x) {
@@ -420,8 +426,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         }
         if (lane < 32) {
           kscale[lane] = ks;
-          // below 2^-110 the reference no longer follows, the weight still does
-          vlog[lane] = fmaxf(log2f(vs), -110.0f);
+          vlog[lane] = fmaxf(log2f(vs), kLeastLog);
           vscale[lane] = vs;
         }
       }
@@ -856,8 +861,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
         }
         float *sc = (float *)(smem + 4 * M::side + ((t + 1) & 1) * M::scales);
         sc[lane] = ks;
-        // below 2^-110 the reference no longer follows, the weight still does
-        sc[M::keys + lane] = fmaxf(log2f(vs), -110.0f);
+        sc[M::keys + lane] = fmaxf(log2f(vs), kLeastLog);
         sc[2 * M::keys + lane] = vs;
       }
     } else {

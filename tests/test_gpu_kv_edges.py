@@ -87,3 +87,23 @@ def test_windows_without_end(kv, q, m, causal):
             assert torch.equal(got, want) and torch.equal(other, lse), window
 
 
+@pytest.mark.parametrize("ctype", [E4, I8])
+@pytest.mark.parametrize("n", [1, 70])
+def test_log_sum_of_values_that_are_all_zero(kv, ctype, n):
+    """300,001 keys of one score, whose values are stored as zeros with scale 0:
+    the log-sum is ln(keys).  The sum is exact (equal powers of two, fewer than
+    2^24); the reference and the logarithm of the sum are below 128, each rounded
+    to 2^-18 or, the logarithm, off by 2^-17."""
+    m, page = 300001, 64
+    cache = kv.Cache.empty(-(-m // page), page, 1, 64, ctype)
+    pages = torch.arange(cache.pages, dtype=torch.int32, device="cuda")[None]
+    q = torch.randn(n, 1, 64, generator=torch.Generator().manual_seed(n)).bfloat16().cuda()
+    starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([m], dtype=torch.int32, device="cuda")
+    for bound in (m, 100):
+        out, lse = kv.attention(q, cache, pages, starts, lens, causal=False, max_kv_len=bound,
+                                return_lse=True)
+        assert bool((out == 0).all())
+        assert float((lse.double() - math.log(m)).abs().max()) <= 2.0 ** -16, bound
+
+
