@@ -426,7 +426,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         }
         if (lane < 32) {
           kscale[lane] = ks;
-          vlog[lane] = fmaxf(log2f(vs), kLeastLog);
+          vlog[lane] = fmaxf(log2f(fabsf(vs)), kLeastLog);
           vscale[lane] = vs;
         }
       }
@@ -861,7 +861,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
         }
         float *sc = (float *)(smem + 4 * M::side + ((t + 1) & 1) * M::scales);
         sc[lane] = ks;
-        sc[M::keys + lane] = fmaxf(log2f(vs), kLeastLog);
+        sc[M::keys + lane] = fmaxf(log2f(fabsf(vs)), kLeastLog);
         sc[2 * M::keys + lane] = vs;
       }
     } else {

@@ -107,3 +107,25 @@ def test_log_sum_of_values_that_are_all_zero(kv, ctype, n):
         assert float((lse.double() - math.log(m)).abs().max()) <= 2.0 ** -16, bound
 
 
+@pytest.mark.parametrize("ctype", [E4, I8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scales_of_either_sign(kv, ctype, dim):
+    """An element stands for code * scale, whatever the scale's sign; the log-sum
+    does not depend on the values.  (The outputs themselves are not negated bit
+    for bit: a matrix product's own rounding depends on the sign.)"""
+    s = make(kv, [1, 100], [90, 300], 4, 2, dim, 16, ctype, BF)
+    c = s["cache"]
+    args = s["q"], c, s["pages"], s["starts"], s["kv_lens"]
+    _, lse = kv.attention(*args, return_lse=True)
+    c.v_scale.neg_()
+    check(kv, s, "negative scales of values")
+    assert torch.equal(kv.attention(*args, return_lse=True)[1], lse)
+    c.v_scale.neg_()
+    c.k_scale.neg_()
+    check(kv, s, "negative scales of keys")
+    c.k_scale.neg_()
+    c.v_scale[:, :, ::3] *= -1
+    c.k_scale[:, :, ::5] *= -1
+    check(kv, s, "scales of both signs")
+
+
