@@ -129,3 +129,16 @@ def test_scales_of_either_sign(kv, ctype, dim):
     check(kv, s, "scales of both signs")
 
 
+@pytest.mark.parametrize("ctype,qtype", [(BF, BF), (E4, BF), (I8, FP)])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_more_than_64_requests(kv, ctype, qtype, dim):
+    """Requests are found 64 at a time: 200 of them, with prompts of many rows,
+    some of them in parts that are joined, and empty ones in between."""
+    q = [(1, 0, 20, 3, 9, 40, 1)[b % 7] for b in range(200)]
+    m = [q[b] + (0, 5, 300, 17, 64)[b % 5] for b in range(200)]
+    for b in (65, 130, 194):
+        q[b], m[b] = 30, 1300
+    s = make(kv, q, m, 2, 1, dim, 16, ctype, qtype)
+    check(kv, s, f"200 requests {ctype} {dim}")
+
+
