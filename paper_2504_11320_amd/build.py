@@ -2,10 +2,13 @@
 
 Each source is compiled to an object in parallel, then the objects are
 linked into one shared library.  Beside it comes _kv.so, the Python module
-with the argument checks of the KV-path operators (host code over PyTorch)."""
+with the argument checks of the KV-path operators (host code over PyTorch).
+The library needs hipcc alone: where what the module needs is not there, or the
+module does not compile, it is built all the same."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -66,11 +69,29 @@ SANITIZE_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitiz
                   "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-g"]
 
 
+def cxx() -> str:
+    return os.environ.get("CXX", "g++")
+
+
+def binding_lacks() -> str:
+    """What building the module takes and this machine does not have."""
+    lacks = []
+    try:
+        import torch  # noqa: F401
+    except ImportError:
+        lacks.append("PyTorch")
+    if not os.path.exists(os.path.join(sysconfig.get_path("include"), "Python.h")):
+        lacks.append("Python's headers")
+    if not shutil.which(cxx()):
+        lacks.append(f"a C++ compiler ({cxx()})")
+    return ", ".join(lacks)
+
+
 def build_binding(verbose: bool = False, out: str = BINDING) -> str:
     """Compile the module of csrc/kv_binding.cpp against the installed PyTorch."""
     import torch
     at = os.path.dirname(torch.__file__)
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+    cmd = [cxx(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INC,
            "-I", sysconfig.get_path("include"), "-isystem", os.path.join(at, "include"),
            "-o", out + ".tmp", os.path.join(CSRC, "kv_binding.cpp"),
@@ -84,9 +105,10 @@ def build_binding(verbose: bool = False, out: str = BINDING) -> str:
 
 def build(verbose: bool = False, defines=(), out: str = LIB, sanitize: bool = False) -> str:
     """Compile every source for gfx950 and link `out` (default: the in-tree
-    library; then the module beside it is compiled too).  `defines` are extra
-    -D options; `sanitize` instruments the host code with ASan and UBSan (load
-    the result with the clang ASan runtime preloaded)."""
+    library; then the module beside it is compiled too, and an error of that is
+    raised once the library is linked).  `defines` are extra -D options;
+    `sanitize` instruments the host code with ASan and UBSan (load the result
+    with the clang ASan runtime preloaded)."""
     dflags = [f"-D{d}" for d in defines] + (SANITIZE_FLAGS if sanitize else [])
     with tempfile.TemporaryDirectory(prefix="wait_sim_build_") as tmp:
         def compile_one(src: str):
@@ -101,11 +123,10 @@ def build(verbose: bool = False, defines=(), out: str = LIB, sanitize: bool = Fa
             return obj
 
         workers = max(1, min(len(SRCS), os.cpu_count() or 1))
+        lacks = binding_lacks() if out == LIB else ""
         with ThreadPoolExecutor(workers) as ex:
-            beside = ex.submit(build_binding, verbose) if out == LIB else None
+            beside = ex.submit(build_binding, verbose, BINDING) if out == LIB and not lacks else None
             objs = list(ex.map(compile_one, SRCS))
-            if beside:
-                beside.result()
         cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out + ".tmp"] + objs
         if sanitize:
             cmd += ["-fsanitize=address,undefined", "-shared-libasan"]
@@ -113,6 +134,15 @@ def build(verbose: bool = False, defines=(), out: str = LIB, sanitize: bool = Fa
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
     os.replace(out + ".tmp", out)
+    failed = beside.exception() if beside else None
+    # an earlier build's module may not fit this library
+    if (lacks or failed) and os.path.exists(BINDING):
+        os.remove(BINDING)
+    if failed:
+        raise failed
+    if lacks:
+        print(f"{os.path.basename(BINDING)}, the module behind kv.py, is not built: it takes {lacks}",
+              file=sys.stderr, flush=True)
     return out
 
 
