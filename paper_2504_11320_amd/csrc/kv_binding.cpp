@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/util/Float8_e4m3fn.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -75,6 +76,14 @@ const at::Tensor *tensor_or_none(PyObject *o, const char *name) {
   return o == Py_None ? nullptr : &tensor(o, name);
 }
 
+// Results carry no gradients, so inputs that ask for them are refused rather than
+// cut off.
+void no_gradient(const at::Tensor &t, const char *name) {
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    refuse("%s requires a gradient, which these operators do not carry (detach it, or call under "
+           "torch.no_grad())", name);
+}
+
 int kv_type(at::ScalarType t) {
   switch (t) {
     case at::kBFloat16: return WS_KV_BF16;
@@ -91,6 +100,7 @@ int index_of(const at::Tensor &t) { return t.is_cuda() ? (int)t.get_device() : -
 
 // [tokens, heads, dim] on GPU `index`.
 ws_kv_rows rows(const at::Tensor &t, const char *name, int index) {
+  no_gradient(t, name);
   if (t.dim() != 3) refuse("%s must be [tokens, heads, dim]", name);
   const int type = kv_type(t.scalar_type());
   if (!wide(type)) refuse("%s must be bf16, fp16 or fp32", name);
@@ -117,6 +127,7 @@ void apart(const at::Tensor &t, const char *name) {
 ws_kv_turn turn(const at::Tensor *positions, const at::Tensor *table, int64_t n, int64_t dim,
                 bool interleaved, int index) {
   need(positions && table, "a rotation needs positions and a table");
+  no_gradient(*table, "table");
   need(table->dim() == 2 && table->scalar_type() == at::kFloat && table->is_contiguous(),
        "table must be [positions, part], fp32, contiguous");
   need(positions->dim() == 1 && positions->size(0) == n && positions->is_contiguous() &&
@@ -246,6 +257,9 @@ PyObject *cache(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
          "int8, contiguous, on one device");
     for (int i = 0; i < 4; ++i) need(k.size(i) <= INT32_MAX, "the cache is too large");
     const at::Tensor *scale[2] = {tensor_or_none(v[2], "k_scale"), tensor_or_none(v[3], "v_scale")};
+    // a cache outlives the mode that it is made in
+    for (auto *t : {&k, &w, scale[0], scale[1]})
+      need(!t || !t->requires_grad(), "a cache's tensors must not require a gradient");
     float *p[2] = {nullptr, nullptr};
     if (type == WS_KV_FP8 || type == WS_KV_INT8) {
       for (int i = 0; i < 2; ++i) {

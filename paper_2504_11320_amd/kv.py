@@ -9,7 +9,10 @@ allocates buffers and supplies the stream).
 * ``attention``: every token's attention over its request's pages.
 
 Every function runs asynchronously on the current stream of its tensors'
-device and needs the HIP library: there is no fallback.
+device and needs the HIP library: there is no fallback.  Results carry no
+gradients, and tensors that require one are refused where autograd records (a
+rotation's gradient is ``rotary`` with ``inverse``, to be called from the
+backward of a ``torch.autograd.Function``).
 """
 from __future__ import annotations
 

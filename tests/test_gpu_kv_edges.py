@@ -142,3 +142,28 @@ def test_more_than_64_requests(kv, ctype, qtype, dim):
     check(kv, s, f"200 requests {ctype} {dim}")
 
 
+def test_rotation_in_an_autograd_function(kv):
+    """The inverse rotation as the backward of a rotation: <rotary(x), w> has the
+    gradient inverse(w), exactly what the call gives."""
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, pos, table):
+            ctx.save_for_backward(pos, table)
+            return kv.rotary(x, pos, table)
+
+        @staticmethod
+        def backward(ctx, g):
+            return kv.rotary(g.contiguous(), *ctx.saved_tensors, inverse=True), None, None
+
+    g = torch.Generator().manual_seed(1)
+    x, w = (torch.randn(7, 3, 64, generator=g).cuda() for _ in range(2))
+    pos, table = torch.arange(7, device="cuda"), kv.rotary_table(20, 32)
+    x.requires_grad_()
+    y = Turn.apply(x, pos, table)
+    assert torch.equal(y.detach(), kv.rotary(x.detach(), pos, table))
+    (y * w).sum().backward()
+    assert torch.equal(x.grad, kv.rotary(w, pos, table, inverse=True))
+    with pytest.raises(ValueError, match="gradient"):
+        kv.rotary(x, pos, table)
+
+
