@@ -84,6 +84,12 @@ void no_gradient(const at::Tensor &t, const char *name) {
            "torch.no_grad())", name);
 }
 
+// Memory that a call has written counts a version, as PyTorch's own operators in
+// place do, so that autograd does not use what it kept of the old contents.
+void written(const at::Tensor &t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 int kv_type(at::ScalarType t) {
   switch (t) {
     case at::kBFloat16: return WS_KV_BF16;
@@ -237,6 +243,7 @@ PyObject *rotary(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
         return f_rotary(&xr, &o, n, (int32_t)heads, (int32_t)dim, &t, inverse, s);
       });
     if (v[5] != Py_None) {
+      written(out);
       Py_INCREF(v[5]);
       return v[5];
     }
@@ -293,11 +300,13 @@ int64_t slots_of(const at::Tensor &t, int index) {
   return t.size(0);
 }
 
-// append(cache bytes, GPU, k, v, slots, positions or None, table or None, interleaved)
+// append(cache bytes, GPU, k, v, slots, positions or None, table or None, interleaved,
+//        the cache's tensors)
 PyObject *append(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
-  ARGS(8)
+  ARGS(9)
   return guarded([&]() -> PyObject * {
     const ws_kv_cache c = cache_of(v[0]);
+    need(PyTuple_Check(v[8]), "not a cache");
     const int index = (int)whole(v[1]);
     const at::Tensor &k = tensor(v[2], "k"), &w = tensor(v[3], "v"), &slots = tensor(v[4], "slots");
     const ws_kv_rows kr = rows(k, "k", index), wr = rows(w, "v", index);
@@ -313,6 +322,8 @@ PyObject *append(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
     run(index, [&](void *s) {
       return f_append(&c, &kr, &wr, slots.data_ptr<int64_t>(), n, turned ? &t : nullptr, s);
     });
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(v[8]); ++i)
+      if (auto *t = tensor_or_none(PyTuple_GET_ITEM(v[8], i), "the cache's")) written(*t);
     Py_RETURN_NONE;
   });
 }
@@ -350,6 +361,7 @@ PyObject *read(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
       a = THPVariable_Wrap(std::move(out[0]));
       b = THPVariable_Wrap(std::move(out[1]));
     } else {
+      for (const auto &t : out) written(t);
       Py_INCREF(a = v[4]);
       Py_INCREF(b = v[5]);
     }
@@ -462,11 +474,14 @@ PyObject *attention(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
     run(index, [&](void *s) {
       return f_attention(&c, &b, &qr, &o, want_lse ? lse.data_ptr<float>() : nullptr, ptr, have, s);
     });
+    if (v[13] != Py_None) written(tensor(v[13], "workspace"));
     PyObject *a;
-    if (v[12] == Py_None)
+    if (v[12] == Py_None) {
       a = THPVariable_Wrap(std::move(out));
-    else
+    } else {
+      written(out);
       Py_INCREF(a = v[12]);
+    }
     if (!want_lse || !a) return a;
     PyObject *z = THPVariable_Wrap(std::move(lse));
     PyObject *pair = z ? PyTuple_Pack(2, a, z) : nullptr;

@@ -148,7 +148,7 @@ class Cache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
         self._c = _native().cache(k, v, k_scale, v_scale)
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.k, self.v, self.k_scale, self.v_scale = self._tensors = k, v, k_scale, v_scale
         self.pages, self.kv_heads, self.page_size, self.dim = k.shape
         self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
 
@@ -175,7 +175,8 @@ def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
     negative, or behind the cache's end, is left out.  With ``positions`` and
     ``table`` the keys are turned first, as by ``rotary``, without a rounding
     between."""
-    _native().append(cache._c, cache._index, k, v, slots, positions, table, interleaved)
+    _native().append(cache._c, cache._index, k, v, slots, positions, table, interleaved,
+                     cache._tensors)
 
 
 def read(cache: Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,

@@ -167,3 +167,51 @@ def test_rotation_in_an_autograd_function(kv):
         kv.rotary(x, pos, table)
 
 
+@pytest.mark.parametrize("ctype", [BF, E4])
+def test_written_tensors_count_their_versions(kv, ctype):
+    """Memory that a call writes is known to autograd as written: what an earlier
+    product kept for its gradient is not used with other contents."""
+    x = torch.randn(3, 2, 64, device="cuda")
+    pos, table = torch.arange(3, device="cuda"), kv.rotary_table(20, 64)
+    slots = torch.arange(3, device="cuda")
+    c = kv.Cache.empty(2, 16, 2, 64, ctype)
+    mine = [t for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None]
+
+    def kept(t):
+        w = torch.ones((), device="cuda", requires_grad=True)
+        return (w * t).sum()
+
+    def written(before, tensors, call):
+        at = [t._version for t in tensors]
+        call()
+        assert all(t._version > v for t, v in zip(tensors, at))
+        with pytest.raises(RuntimeError, match="inplace"):
+            before.backward()
+
+    y = x.clone()
+    written(kept(y), [y], lambda: kv.rotary(y, pos, table, out=y))
+    base = torch.zeros(4, 2, 64, device="cuda")
+    written(kept(base), [base], lambda: kv.rotary(x, pos, table, out=base[1:]))
+    written(kept(c.k_scale if ctype == E4 else c.k), mine, lambda: kv.append(c, x, x, slots))
+    out = torch.zeros_like(x), torch.zeros_like(x)
+    written(kept(out[1]), out, lambda: kv.read(c, slots, out=out))
+    q = torch.zeros(3, 2, 64, device="cuda", dtype=BF)
+    o = torch.zeros_like(q)
+    batch = (c, torch.arange(2, dtype=torch.int32, device="cuda")[None],
+             torch.tensor([0, 3], dtype=torch.int32, device="cuda"),
+             torch.tensor([3], dtype=torch.int32, device="cuda"))
+    written(kept(o), [o], lambda: kv.attention(q, *batch, out=o))
+    space = torch.zeros(1 << 16, device="cuda")
+    written(kept(space), [space], lambda: kv.attention(q, *batch, out=o, workspace=space))
+    # what is only read keeps its version, and so do tensors without one
+    at = [t._version for t in (x, q, *mine)]
+    kv.attention(q, *batch)
+    kv.read(c, slots)
+    kv.rotary(x, pos, table)
+    assert at == [t._version for t in (x, q, *mine)]
+    with torch.inference_mode():
+        free = kv.Cache.empty(2, 16, 2, 64, ctype)
+    kv.append(free, x, x, slots)
+    assert torch.equal(free.k.view(torch.uint8), c.k.view(torch.uint8))
+
+
