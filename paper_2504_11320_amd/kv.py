@@ -138,19 +138,38 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *,
 # ------------------------------------------------------------------ cache ----
 
 
+def _held(i: int, name: str) -> property:
+    def get(cache):
+        return cache._tensors[i]
+
+    def same(cache, tensor):   # what `cache.k *= 2` assigns
+        if tensor is not cache._tensors[i]:
+            raise AttributeError(f"a cache keeps its {name}: make another one")
+
+    return property(get, same)
+
+
 class Cache:
     """One layer's cache: k and v [pages, kv_heads, page_size, dim], bf16, fp16,
     float8_e4m3fn or int8; 8-bit caches have fp32 scales
     [pages, kv_heads, page_size], an element stands for code * scale.  Token
     slot s is offset s % page_size of page s / page_size.  The page size is a
-    power of two up to 1024, dim 64, 128 or 256."""
+    power of two up to 1024, dim 64, 128 or 256.  The tensors' addresses are
+    kept: they cannot be exchanged, and their memory must stay theirs."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
         self._c = _native().cache(k, v, k_scale, v_scale)
-        self.k, self.v, self.k_scale, self.v_scale = self._tensors = k, v, k_scale, v_scale
-        self.pages, self.kv_heads, self.page_size, self.dim = k.shape
-        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
+        self._tensors, self._index = (k, v, k_scale, v_scale), k.get_device()
+
+    def __reduce__(self):   # copies and pickles have addresses of their own
+        return type(self), self._tensors
+
+    k, v, k_scale, v_scale = (_held(i, n) for i, n in enumerate(("k", "v", "k_scale", "v_scale")))
+    pages, kv_heads, page_size, dim = (property(lambda self, i=i: self._tensors[0].shape[i])
+                                       for i in range(4))
+    dtype = property(lambda self: self._tensors[0].dtype)
+    device = property(lambda self: self._tensors[0].device)
 
     @classmethod
     def empty(cls, pages: int, page_size: int, kv_heads: int, dim: int,

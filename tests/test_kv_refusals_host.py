@@ -1,5 +1,8 @@
 """What the KV-path operators' Python calls refuse: gradients, memory that
 overlaps, replaced tensors of a cache.  No GPU: the checks come first."""
+import copy
+import pickle
+
 import pytest
 import torch
 
@@ -56,5 +59,38 @@ def test_a_cache_of_parameters_is_refused():
     c, s = torch.zeros(4, 2, 16, 64, dtype=torch.int8), torch.zeros(4, 2, 16)
     with pytest.raises(ValueError, match="gradient"):
         kv.Cache(c, c.clone(), s, s.clone().requires_grad_())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+def test_a_caches_tensors_stay(dtype):
+    """The addresses of a cache's memory are kept beside its tensors, so these
+    cannot be exchanged or taken away; operations in place can be written as
+    assignments."""
+    c = small(dtype)
+    before = c.k, c.v, c.k_scale, c.v_scale
+    for name in ("k", "v", "k_scale", "v_scale"):
+        t = getattr(c, name)
+        for other in (None if t is not None else torch.zeros(4, 2, 16), torch.zeros(4, 2, 16, 64),
+                      None if t is None else t.clone()):
+            if other is t:
+                continue
+            with pytest.raises(AttributeError):
+                setattr(c, name, other)
+        with pytest.raises(AttributeError):
+            delattr(c, name)
+    for name in ("pages", "kv_heads", "page_size", "dim", "dtype", "device"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, 1)
+    if dtype == torch.int8:
+        c.v_scale += 1.0
+        assert bool((c.v_scale == 1.0).all())
+    assert all(a is b for a, b in zip(before, (c.k, c.v, c.k_scale, c.v_scale)))
+    assert (c.pages, c.kv_heads, c.page_size, c.dim, c.dtype) == (4, 2, 16, 64, dtype)
+    assert c.device == c.k.device
+    # a copy has the addresses of its own tensors
+    for other in (copy.copy(c), copy.deepcopy(c), pickle.loads(pickle.dumps(c))):
+        assert other._c == kv.Cache(other.k, other.v, other.k_scale, other.v_scale)._c
+        assert other.k.dtype == dtype and other.kv_heads == 2
+    assert copy.copy(c).k is c.k and copy.deepcopy(c).k.data_ptr() != c.k.data_ptr()
 
 
