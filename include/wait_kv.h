@@ -18,7 +18,8 @@
  * wait_sim_last_error().  Strides are in elements; a vector's own elements lie
  * one after another.  Vectors whose base or strides are not multiples of 16
  * bytes take slower loads, with the same results.  Output rows must not
- * overlap one another.
+ * overlap one another, nor an input's rows; those of wait_kv_rotary and
+ * wait_kv_attention may be the input itself.
  */
 #ifndef WAIT_KV_H
 #define WAIT_KV_H
@@ -69,8 +70,9 @@ typedef struct {
 } ws_kv_cache;
 
 /* out = x turned; inverse: turned back (the gradient of a rotation).  n tokens
- * of `heads` vectors of dim elements; out may be x itself.  Angles and products
- * are in fp32, rounded once to x's type. */
+ * of `heads` vectors of dim elements; out may be x itself, and shares no memory
+ * with it otherwise (rows within the range of the other's need the same token
+ * stride).  Angles and products are in fp32, rounded once to x's type. */
 int wait_kv_rotary(const ws_kv_rows *x, const ws_kv_rows *out, int64_t n, int32_t heads,
                    int32_t dim, const ws_kv_turn *turn, int32_t inverse, void *hip_stream);
 
@@ -121,7 +123,8 @@ typedef struct {
 int wait_kv_attention_workspace_bytes(const ws_kv_cache *cache, const ws_kv_batch *batch,
                                       size_t *bytes);
 
-/* q and out: bf16 or fp16, the cache's type where that is a 16-bit one.
+/* q and out: bf16 or fp16, the cache's type where that is a 16-bit one; out may
+ * be q itself, and shares no memory with it otherwise (as in wait_kv_rotary).
  * lse (NULL: none): [n_tokens][heads] fp32, the natural logarithm of the
  * softmax's denominator, sum_j exp(scale q . k_j).  Products, softmax and sums
  * are in fp32; the weights are rounded to 16 bits before they meet the

@@ -1400,6 +1400,8 @@ int wait_kv_attention(const ws_kv_cache *cache, const ws_kv_batch *batch, const 
       return invalid("attention: q and out must both be bf16 or both fp16");
     if (!is_8bit(cache->type) && q->type != cache->type)
       return invalid("attention: q must have the type of a 16-bit cache");
+    if (!one_place(*q, *out) && overlap(*q, *out, b.n_tokens, b.heads, cache->dim))
+      return invalid("attention: out must be q or not overlap it");
     if ((uintptr_t)lse % 4) return invalid("attention: lse must be aligned to 4 bytes");
     if (b.n_seq == 0 || b.n_tokens == 0) return WS_OK;
     if (!b.starts || !b.kv_lens || (b.table_cols > 0 && !b.table))

@@ -538,6 +538,8 @@ int wait_kv_rotary(const ws_kv_rows *x, const ws_kv_rows *out, int64_t n, int32_
     if (x->data == out->data &&
         (x->token_stride != out->token_stride || x->head_stride != out->head_stride))
       return invalid("rotary: in place, the strides must be the same");
+    if (!one_place(*x, *out) && overlap(*x, *out, n, heads, dim))
+      return invalid("rotary: out must be x or not overlap it");
     if (n == 0) return WS_OK;
     RotaryArgs a{};
     a.x = x->data;
@@ -613,6 +615,8 @@ int wait_kv_read(const ws_kv_cache *cache, const int64_t *slots, int64_t n, cons
     if (int rc = check_rows(k, n, "read: k must be non-NULL")) return rc;
     if (int rc = check_rows(v, n, "read: v must be non-NULL")) return rc;
     if (k->type != v->type) return invalid("read: k and v must have one type");
+    if (overlap(*k, *v, n, cache->kv_heads, cache->dim))
+      return invalid("read: k and v must not overlap");
     if (n > 0 && !slots) return invalid("read: slots must be non-NULL");
     if ((uintptr_t)slots % 8) return invalid("read: slots must be aligned to 8 bytes");
     if (n == 0) return WS_OK;

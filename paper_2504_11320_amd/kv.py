@@ -130,8 +130,8 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *,
     """x [tokens, heads, dim] with the first ``table.shape[1]`` elements of
     every vector turned by the token's position: pairs (i, i + part / 2), or
     (2 i, 2 i + 1) where ``interleaved``.  ``inverse`` turns back; that is the
-    gradient's way through a rotation.  ``out`` may be x.  A position outside
-    the table gives NaN."""
+    gradient's way through a rotation.  ``out`` may be x, and must not overlap
+    it otherwise.  A position outside the table gives NaN."""
     return _native().rotary(x, positions, table, interleaved, inverse, out)
 
 
@@ -226,7 +226,9 @@ def attention(q: torch.Tensor, cache: Cache, pages: torch.Tensor, starts: torch.
     ``starts``, ``kv_lens`` and ``pages`` are int32 and stay on the device;
     ``max_q_len`` and ``max_kv_len`` bound the lengths for the launch's layout
     (by default from the shapes) and longer requests are only slower.
-    Returns out, or (out, lse [tokens, heads] fp32).  ``workspace`` (a uint8
+    Returns out, or (out, lse [tokens, heads] fp32); rows of queries outside every
+    request stay as they are in a given ``out``, and are undefined otherwise.
+    ``out`` may be q, and must not overlap it otherwise.  ``workspace`` (a uint8
     tensor of ``attention_workspace_bytes``) is taken from PyTorch where it is
     not given."""
     return _native().attention(cache._c, cache._index, q, pages, starts, kv_lens, max_q_len,

@@ -215,3 +215,47 @@ def test_written_tensors_count_their_versions(kv, ctype):
     assert torch.equal(free.k.view(torch.uint8), c.k.view(torch.uint8))
 
 
+def test_rows_beside_one_another(kv):
+    """Parts of one buffer's rows as input and output, which lie within one
+    another's range and share nothing; an output that is the input."""
+    T, H, D = 40, 4, 64
+    g = torch.Generator().manual_seed(3)
+    buf = torch.randn(T, 3, H, D, generator=g).to(BF).cuda()
+    pos, table = torch.arange(T, device="cuda"), kv.rotary_table(T, D)
+    x = buf[:, 0].clone()
+    want = kv.rotary(x, pos, table)
+    for out in (buf[:, 1], buf[:, 2]):
+        assert torch.equal(kv.rotary(buf[:, 0], pos, table, out=out), want)
+    assert torch.equal(buf[:, 0], x)
+    wide = torch.zeros(T, 2 * H, D, dtype=BF, device="cuda")   # every other head
+    wide[:, ::2] = x
+    assert torch.equal(kv.rotary(wide[:, ::2], pos, table, out=wide[:, 1::2]), want)
+    assert torch.equal(wide[:, ::2], x)
+    heads = torch.zeros(2, H, T, D, dtype=BF, device="cuda")   # heads outside, side by side
+    heads[0] = x.transpose(0, 1)
+    a, b = (t.transpose(0, 1) for t in heads)
+    assert torch.equal(kv.rotary(a, pos, table, out=b), want)
+    thin = torch.zeros(T, H, 2, D, dtype=BF, device="cuda")    # other strides, between
+    thin[:, :, 0] = x
+    assert torch.equal(kv.rotary(thin[:, :, 0], pos, table, out=thin[:, :, 1]), want)
+    for bad in ((buf[1:, 0], buf[:-1, 0]), (wide[:, :H], wide[:, 1:H + 1]),
+                (x[:1].expand(T, -1, -1), x)):
+        with pytest.raises((ValueError, RuntimeError)):
+            kv.rotary(bad[0], pos[:bad[0].shape[0]], table, out=bad[1])
+    c = kv.Cache.empty(3, 16, H, D, BF)
+    slots = torch.arange(T, device="cuda")
+    kv.append(c, x, want, slots)
+    k, v = kv.read(c, slots, out=(buf[:, 1], buf[:, 2]))
+    assert torch.equal(k, x) and torch.equal(v, want)
+    with pytest.raises((ValueError, RuntimeError)):
+        kv.read(c, slots, out=(x, x))
+    for q_lens, kv_lens in (([1, 1], [40, 33]), ([30, 9], [48, 40]), ([1, 36], [3000, 700])):
+        s = make(kv, q_lens, kv_lens, H, 2, D, 16, E4, BF)
+        args = s["cache"], s["pages"], s["starts"], s["kv_lens"]
+        got = kv.attention(s["q"], *args)
+        n = got.shape[0]
+        buf[:n, 0] = s["q"]
+        assert torch.equal(kv.attention(buf[:n, 0], *args, out=buf[:n, 2]), got)
+        assert torch.equal(kv.attention(buf[:n, 0], *args, out=buf[:n, 0]), got)
+
+

@@ -6,6 +6,7 @@ import pickle
 import pytest
 import torch
 
+from paper_2504_11320_amd import binding as B
 from paper_2504_11320_amd import kv
 
 
@@ -92,5 +93,49 @@ def test_a_caches_tensors_stay(dtype):
         assert other._c == kv.Cache(other.k, other.v, other.k_scale, other.v_scale)._c
         assert other.k.dtype == dtype and other.kv_heads == 2
     assert copy.copy(c).k is c.k and copy.deepcopy(c).k.data_ptr() != c.k.data_ptr()
+
+
+FAKE = 1 << 40   # never dereferenced: the checks come first
+
+
+def rows(data, token, head=64, type=kv.BF16):
+    return kv.ROWS.pack(data, token, head, type)
+
+
+# (x's address, token and head stride), (out's): 5 tokens of 2 heads of 64
+OVERLAPS = [((0, 128, 64), (2, 128, 64)),            # one element on
+            ((0, 128, 64), (256, 128, 64)),          # one token on
+            ((256, 128, 64), (0, 128, 64)),
+            ((0, 128, 64), (128, 128, 64)),          # one head on
+            ((0, 384, 64), (128, 384, 64)),          # the same within wider rows
+            ((0, 384, 64), (254, 384, 64)),          # one element of the second head
+            ((0, 384, 64), (768 * 4, 384, 64)),      # the last token alone
+            ((0, 64, 320), (128, 64, 320)),          # heads outside
+            ((0, 384, 64), (0, 384, 128)),           # other heads' stride
+            ((0, 384, 64), (-768 * 2, 384, 128)),
+            ((0, 128, 64), (0, 64, 320)),            # one base, transposed
+            ((0, 128, 64), (64, 256, 64)),
+            ((1024, -128, 64), (0, 128, 64))]        # backwards
+
+
+@pytest.mark.parametrize("x,out", OVERLAPS)
+def test_overlapping_memory_is_refused(x, out):
+    """An output that shares memory with the input, unless it is the input
+    itself, or with the other output."""
+    L = kv._lib()
+    a, b = (rows(FAKE + at, token, head) for at, token, head in (x, out))
+    turn = kv.TURN.pack(FAKE, FAKE, 0, 10, 32, 0)
+    cache = kv.CACHE.pack(FAKE, FAKE, 0, 0, 4, 16, 2, 64, kv.BF16)
+    batch = kv.BATCH.pack(FAKE, 8, 8, FAKE, FAKE, 1, 5, 2, 1.0, 1, 0, 5, 100)
+    big = 1 << 30
+    for p, q in ((a, b), (b, a)):
+        assert L.wait_kv_rotary(p, q, 5, 2, 64, turn, 0, None) == B.WS_EINVAL
+        assert b"overlap" in L.wait_sim_last_error() or b"in place" in L.wait_sim_last_error()
+        assert L.wait_kv_read(cache, FAKE, 5, p, q, None) == B.WS_EINVAL
+        assert b"overlap" in L.wait_sim_last_error()
+        assert L.wait_kv_attention(cache, batch, p, q, None, FAKE, big, None) == B.WS_EINVAL
+        assert b"overlap" in L.wait_sim_last_error()
+    same = rows(FAKE, 128)
+    assert L.wait_kv_read(cache, FAKE, 5, same, same, None) == B.WS_EINVAL
 
 
