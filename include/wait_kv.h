@@ -77,7 +77,9 @@ int wait_kv_rotary(const ws_kv_rows *x, const ws_kv_rows *out, int64_t n, int32_
                    int32_t dim, const ws_kv_turn *turn, int32_t inverse, void *hip_stream);
 
 /* Rows i = 0 .. n-1 of k and v into slots[i] (int64); a row whose slot is
- * outside the cache is left out.  Two rows with one slot leave either.
+ * outside the cache is left out.  Slots within the cache must differ: what two
+ * rows with one slot leave there is made of both, codes of one under the scale
+ * of the other among it.
  * turn (NULL: none) rotates k.  8-bit types: with t the row's largest
  * magnitude and M the largest code (448, 127), scale = t / M and
  * code = x * ((1 / t) * M) in fp32, rounded to nearest, ties to even.  Rows

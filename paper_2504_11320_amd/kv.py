@@ -191,7 +191,8 @@ def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
            interleaved: bool = False) -> None:
     """Rows of k and v [tokens, kv_heads, dim] into the cache's slots, rounded
     or quantised row by row (include/wait_kv.h).  A token whose slot is
-    negative, or behind the cache's end, is left out.  With ``positions`` and
+    negative, or behind the cache's end, is left out; the other slots must differ
+    (two tokens with one slot leave a mixture of both).  With ``positions`` and
     ``table`` the keys are turned first, as by ``rotary``, without a rounding
     between."""
     _native().append(cache._c, cache._index, k, v, slots, positions, table, interleaved,

@@ -1,12 +1,14 @@
 """What the KV-path operators' Python calls refuse: gradients, memory that
 overlaps, replaced tensors of a cache.  No GPU: the checks come first."""
 import copy
+import os
 import pickle
 
 import pytest
 import torch
 
 from paper_2504_11320_amd import binding as B
+from paper_2504_11320_amd import build as Bd
 from paper_2504_11320_amd import kv
 
 
@@ -137,5 +139,15 @@ def test_overlapping_memory_is_refused(x, out):
         assert b"overlap" in L.wait_sim_last_error()
     same = rows(FAKE, 128)
     assert L.wait_kv_read(cache, FAKE, 5, same, same, None) == B.WS_EINVAL
+
+
+def test_nothing_is_promised_of_one_slot_twice():
+    """Codes and scale of a row are separate stores of several lanes: the
+    documents must not promise one of the rows."""
+    src = open(os.path.join(Bd.INC, "wait_kv.h")).read()
+    text = " ".join(src.replace("*", " ").split())
+    assert "leave either" not in text
+    assert "Slots within the cache must differ" in text
+    assert "slots must differ" in " ".join(kv.append.__doc__.split())
 
 
