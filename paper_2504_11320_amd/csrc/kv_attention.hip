@@ -41,11 +41,12 @@ struct Args {
   int32_t causal, window;
   int32_t q_bf16;
   // results of parts, the sums o and (m, l): few rows [request][KV head]
-  // [few_blocks * 16][part], many rows [token][head][part]
+  // [few_room][part], many rows [token][head][part]
   float *few_o, *many_o;
   float2 *few_ml, *many_ml;
   int32_t few_splits, few_chunk;    // of a few-rows launch: parts, keys a part
-  int32_t few_blocks;               // and row blocks of a request
+  int32_t few_blocks;               // row blocks of a request
+  int32_t few_room;                 // rows of a request that may have parts
   int32_t many_splits, many_chunk;  // of a many-rows launch
   int32_t both;          // requests of more than 16 rows are the many-rows blocks'
   int32_t row_blocks;    // numbers of row blocks of the many-rows launch
@@ -119,7 +120,7 @@ __device__ __forceinline__ int32_t parts_of(Range r, int32_t chunk, int32_t spli
 // The parts of a few-rows block.  A request that has more rows than its launch
 // was laid out for has no room for parts.
 __device__ __forceinline__ int32_t few_parts(const Args &a, Range r, int32_t rows) {
-  return rows > kFewRows * a.few_blocks ? 1 : parts_of(r, a.few_chunk, a.few_splits);
+  return rows > a.few_room ? 1 : parts_of(r, a.few_chunk, a.few_splits);
 }
 
 // Key j of a request, 0 < end: its page's entry in the table, read ahead (the
@@ -595,7 +596,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         if (a.lse && d == 0) a.lse[q_row * a.heads + hd] = natural_lse(top, total);
       } else {
         const int64_t to =
-            ((int64_t)(b * a.kv_heads + h) * a.few_blocks * kFewRows + r0 + r) * a.few_splits + split;
+            ((int64_t)(b * a.kv_heads + h) * a.few_room + r0 + r) * a.few_splits + split;
         *reinterpret_cast<f32x4 *>(a.few_o + to * D + d) = x;
         if (d == 0) a.few_ml[to] = make_float2(top, total);
       }
@@ -1193,8 +1194,8 @@ __device__ __forceinline__ void join_few(const Args &a, int32_t id, int32_t nth,
   const int32_t head = id % a.heads, b = id / a.heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
-  if (rows == 0 || rows > kFewRows * a.few_blocks) return;
-  const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * a.few_blocks * kFewRows;
+  if (rows == 0 || rows > a.few_room) return;
+  const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * a.few_room;
   for (int32_t i = nth; i < s.n; i += step) {
     const int32_t row = i * a.group + head % a.group, r0 = row / kFewRows * kFewRows;
     const int32_t parts =
@@ -1252,7 +1253,7 @@ __global__ void __launch_bounds__(256) join_kernel(Args a, int32_t few, int32_t 
 // How a batch is laid out over workgroups.
 struct Layout {
   bool many, wide;
-  int32_t few_splits, few_chunk, few_blocks, many_splits, many_chunk, row_blocks;
+  int32_t few_splits, few_chunk, few_blocks, few_room, many_splits, many_chunk, row_blocks;
   int64_t few_slots, many_slots;  // results of parts in the workspace
   int64_t bytes;
 };
@@ -1289,6 +1290,7 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // keys they are not: 32 prompts of 30 to 60 tokens 47 us against 33.
   L.many = max_rows > 4 * kFewRows || (max_rows > kFewRows && max_kv < 16 * max_rows);
   L.few_blocks = L.many ? 1 : (int32_t)ceil_div(max_rows, kFewRows);
+  L.few_room = L.many ? kFewRows : (int32_t)max_rows;
   const int64_t many_rows = c.dim == 256 ? kManyRows<256> : kManyRows<128>;
   int64_t few_keys = max_kv, many_keys = max_kv;
   if (b.window) {
@@ -1309,7 +1311,7 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // over 4 heads 31 us with 512 and 25 with 256.  D = 256 has tiles of 32 keys.
   const int64_t least = (full >= 64 ? 512 : 256) / (c.dim == 256 ? 2 : 1);
   split_keys(many_keys, full, 256, least, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
-  if (L.few_splits > 1) L.few_slots = pairs * kFewRows * L.few_blocks * L.few_splits;
+  if (L.few_splits > 1) L.few_slots = pairs * L.few_room * L.few_splits;
   if (L.many && L.many_splits > 1)
     L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
   L.bytes = (L.few_slots + L.many_slots) * (c.dim + 2) * 4;
@@ -1353,7 +1355,7 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   if (int rc = launched()) return rc;
   if (L.bytes) {
     // a request whose few rows have parts has at most so many tokens
-    const int32_t step = std::max(1, L.few_blocks * kFewRows / a.group);
+    const int32_t step = std::max(1, L.few_room / a.group);
     const int64_t few = L.few_slots ? (int64_t)a.n_seq * a.heads * step : 0;
     constexpr int several = 64 / kJoinLanes<D>;
     const int64_t waves = (int64_t)a.n_tokens * ceil_div(a.heads, several);
@@ -1449,6 +1451,7 @@ int wait_kv_attention(const ws_kv_cache *cache, const ws_kv_batch *batch, const 
     a.few_splits = L.few_splits;
     a.few_chunk = L.few_chunk;
     a.few_blocks = L.few_blocks;
+    a.few_room = L.few_room;
     a.many_splits = L.many_splits;
     a.many_chunk = L.many_chunk;
     a.both = L.many;

@@ -51,3 +51,20 @@ def test_prompts_in_parts(kv, ctype, dim):
     s = make(kv, [40, 1, 3], [2600, 4100, 1900], 10, 2, dim, 16, ctype, FP)
     held(kv, s, f"prompts {ctype} {dim}", ({}, dict(max_q_len=1), dict(max_kv_len=700)))
     held(kv, s, f"prompts {ctype} {dim}, not causal", causal=False)
+
+
+@pytest.mark.parametrize("group", [1, 4])
+@pytest.mark.parametrize("ctype", [E4, I8])
+def test_requests_longer_than_laid_out(kv, ctype, group):
+    """Rows that have room for parts beside rows that have none, in a workspace
+    of exactly the bytes asked for."""
+    s = make(kv, [1, 2, 4, 1, 3], [3000, 2900, 4100, 1800, 2600], 2 * group, 2, 128, 16, ctype, FP)
+    args = s["q"], s["cache"], s["pages"], s["starts"], s["kv_lens"]
+    o, tol = attend_codes(*args)
+    assert says_something(o, tol)
+    for n in (1, 2, 3, 4, 9, None):
+        size = kv.attention_workspace_bytes(*args, max_q_len=n)
+        space = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        got = kv.attention(*args, max_q_len=n, workspace=space[:size])
+        within(got, o, tol, f"laid out for {n}")
+        assert size > 0 and bool((space[size:] == 0xA5).all())

@@ -1,6 +1,7 @@
 """What the KV-path operators' Python calls refuse: gradients, memory that
 overlaps, replaced tensors of a cache.  No GPU: the checks come first."""
 import copy
+import ctypes as C
 import os
 import pickle
 
@@ -149,5 +150,24 @@ def test_nothing_is_promised_of_one_slot_twice():
     assert "leave either" not in text
     assert "Slots within the cache must differ" in text
     assert "slots must differ" in " ".join(kv.append.__doc__.split())
+
+
+def test_workspace_of_loose_bounds():
+    """Rows that a batch cannot have take no room in the workspace: 128 single
+    tokens of 32 heads over a table of 131,072 keys, where each may have 32 parts."""
+    cache = kv.CACHE.pack(FAKE, FAKE, FAKE, FAKE, 8192, 16, 32, 128, kv.INT8)
+
+    def size(max_q, heads=32, tokens=128, cols=8192):
+        batch = kv.BATCH.pack(FAKE, cols, cols, FAKE, FAKE, 128, tokens, heads, 1.0, 1, 0, max_q,
+                              cols * 16)
+        n = C.c_size_t()
+        assert kv._lib().wait_kv_attention_workspace_bytes(cache, batch, n) == B.WS_OK
+        return n.value
+
+    one = 32 * (128 + 2) * 4           # the parts of a row
+    assert size(1) == 128 * 32 * one < 100e6
+    assert size(1, cols=2048) == 128 * 32 * 8 * (128 + 2) * 4
+    assert size(1, heads=64) == 128 * 64 * one
+    assert size(5, heads=64, tokens=640) == 128 * 32 * 10 * one
 
 
