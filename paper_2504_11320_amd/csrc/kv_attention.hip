@@ -1339,13 +1339,19 @@ int check_batch(const ws_kv_cache *c, const ws_kv_batch *b) {
 template <int TYPE, int D>
 int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
   const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
-  const int64_t few = pairs * L.few_splits * L.few_blocks, many = (int64_t)a.kv_heads * L.many_splits * L.row_blocks;
-  if (few >= (int64_t)1 << 31 || many >= (int64_t)1 << 31)
-    return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
+  const int64_t few = pairs * L.few_splits * L.few_blocks;
+  const int64_t many = L.many ? (int64_t)a.kv_heads * L.many_splits * L.row_blocks : 0;
   constexpr int wide = kWideWaves<D>;
+  // a request whose few rows have parts has at most so many tokens
+  const int32_t step = std::max(1, L.few_room / a.group);
+  const int64_t join_few = L.few_slots ? (int64_t)a.n_seq * a.heads * step : 0;
+  constexpr int several = 64 / kJoinLanes<D>;
+  const int64_t waves = (int64_t)a.n_tokens * ceil_div(a.heads, several);
+  const int64_t join = L.bytes ? join_few + (L.many_slots ? ceil_div(waves, 4) : 0) : 0;
+  // a launch has fewer than 2^32 threads
+  if ((few + many) * 64 * (L.wide ? wide : 4) >= (int64_t)1 << 32 || join * 256 >= (int64_t)1 << 32)
+    return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
   if (L.many) {
-    if (few + many >= (int64_t)1 << 31)
-      return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
     rows_kernel<TYPE, D><<<dim3((uint32_t)(few + many)), 64 * wide, 0, stream>>>(a, (int32_t)many);
   } else if (L.wide) {
     few_rows_kernel<TYPE, D, wide><<<dim3((uint32_t)few), 64 * wide, 0, stream>>>(a);
@@ -1353,17 +1359,9 @@ int attention_launch(const Args &a, const Layout &L, hipStream_t stream) {
     few_rows_kernel<TYPE, D, 4><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
   }
   if (int rc = launched()) return rc;
-  if (L.bytes) {
-    // a request whose few rows have parts has at most so many tokens
-    const int32_t step = std::max(1, L.few_room / a.group);
-    const int64_t few = L.few_slots ? (int64_t)a.n_seq * a.heads * step : 0;
-    constexpr int several = 64 / kJoinLanes<D>;
-    const int64_t waves = (int64_t)a.n_tokens * ceil_div(a.heads, several);
-    const int64_t blocks = few + (L.many_slots ? ceil_div(waves, 4) : 0);
-    if (blocks >= (int64_t)1 << 31)
-      return ws_record_failure(WS_EUNSUPPORTED, "attention: too many workgroups");
-    join_kernel<D><<<dim3((uint32_t)blocks), 256, 0, stream>>>(a, (int32_t)few, step,
-                                                               Many<TYPE, D>::keys);
+  if (join) {
+    join_kernel<D><<<dim3((uint32_t)join), 256, 0, stream>>>(a, (int32_t)join_few, step,
+                                                             Many<TYPE, D>::keys);
     return launched();
   }
   return WS_OK;

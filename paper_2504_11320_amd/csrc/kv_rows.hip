@@ -131,22 +131,34 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
   }
 }
 
-// Launches over tokens, each of fewer than 2^31 threads: indexes within one are
-// 32-bit.
-template <class T, class F>
-int in_ranges(RotaryArgs a, int64_t threads_a_token, F &&launch) {
-  const int64_t most = (((int64_t)1 << 31) - 256) / threads_a_token;
-  if (most < 1) return ws_record_failure(WS_EUNSUPPORTED, "rotary: too many elements a token");
-  const int64_t all = a.n;
-  for (int64_t from = 0; from < all; from += most) {
-    a.n = all - from < most ? all - from : most;
-    launch(a, (uint32_t)((a.n * threads_a_token + 255) / 256));
+// Launches over n tokens, of which each has fewer than 2^32 threads, the most that
+// one can have, in whole units of tokens.  launch(from, n) does the tokens
+// from .. from + n - 1.
+template <class F>
+int token_ranges(int64_t n, int64_t threads_a_token, int unit, F &&launch) {
+  const int64_t most = (((int64_t)1 << 32) - 256) / threads_a_token / unit * unit;
+  if (most < 1) return ws_record_failure(WS_EUNSUPPORTED, "too many elements a token");
+  for (int64_t from = 0; from < n; from += most) {
+    launch(from, n - from < most ? n - from : most);
     if (int rc = launched()) return rc;
-    a.x = (const typename T::raw *)a.x + a.n * a.xt;
-    a.out = (typename T::raw *)a.out + a.n * a.ot;
-    a.turn.positions = (const char *)a.turn.positions + a.n * (a.turn.positions_32 ? 4 : 8);
   }
   return WS_OK;
+}
+
+void skip_positions(TurnArgs &t, int64_t n) {
+  if (t.positions) t.positions = (const char *)t.positions + n * (t.positions_32 ? 4 : 8);
+}
+
+template <class T, class F>
+int in_ranges(const RotaryArgs &all, int64_t threads_a_token, F &&launch) {
+  return token_ranges(all.n, threads_a_token, 1, [&](int64_t from, int64_t n) {
+    RotaryArgs a = all;
+    a.n = n;
+    a.x = (const typename T::raw *)a.x + from * a.xt;
+    a.out = (typename T::raw *)a.out + from * a.ot;
+    skip_positions(a.turn, from);
+    launch(a, (uint32_t)((n * threads_a_token + 255) / 256));
+  });
 }
 
 template <class T, int VEC, bool INTER>
@@ -397,16 +409,23 @@ int append_launch(AppendArgs a, int vec, hipStream_t stream) {
   const bool lanes = vec >= wide && !a.interleaved && a.turn.part % 16 == 0;
   const bool many = lanes && a.heads >= kHeads && a.n * a.heads * G > kResidentThreads;
   a.head_groups = many ? (a.heads + kHeads - 1) / kHeads : a.heads;
-  const dim3 blocks((uint32_t)((a.n * a.head_groups + 256 / G - 1) / (256 / G)));
-  if (many)
-    append_kernel<T, TYPE, G, wide, kHeads, true><<<blocks, 256, 0, stream>>>(a);
-  else if (lanes)
-    append_kernel<T, TYPE, G, wide, 1, true><<<blocks, 256, 0, stream>>>(a);
-  else if (vec >= wide)
-    append_kernel<T, TYPE, G, wide, 1, false><<<blocks, 256, 0, stream>>>(a);
-  else
-    append_kernel<T, TYPE, G, 1, 1, false><<<blocks, 256, 0, stream>>>(a);
-  return launched();
+  return token_ranges(a.n, (int64_t)a.head_groups * G, 1, [&](int64_t from, int64_t n) {
+    AppendArgs r = a;
+    r.n = n;
+    r.k = (const typename T::raw *)a.k + from * a.kt;
+    r.v = (const typename T::raw *)a.v + from * a.vt;
+    r.slots = a.slots + from;
+    skip_positions(r.turn, from);
+    const dim3 blocks((uint32_t)((n * a.head_groups + 256 / G - 1) / (256 / G)));
+    if (many)
+      append_kernel<T, TYPE, G, wide, kHeads, true><<<blocks, 256, 0, stream>>>(r);
+    else if (lanes)
+      append_kernel<T, TYPE, G, wide, 1, true><<<blocks, 256, 0, stream>>>(r);
+    else if (vec >= wide)
+      append_kernel<T, TYPE, G, wide, 1, false><<<blocks, 256, 0, stream>>>(r);
+    else
+      append_kernel<T, TYPE, G, 1, 1, false><<<blocks, 256, 0, stream>>>(r);
+  });
 }
 
 template <class T, int TYPE>
@@ -488,14 +507,20 @@ __global__ void __launch_bounds__(256) read_kernel(ReadArgs a) {
 
 template <class T, int TYPE, int G>
 int read_launch(const ReadArgs &a, int vec, hipStream_t stream) {
-  const int64_t rows = (a.n + 15) / 16 * 16 * a.heads;
-  const dim3 blocks((uint32_t)((rows + 256 / G - 1) / (256 / G)));
   constexpr int wide = 16 / sizeof(typename T::raw);
-  if (vec >= wide)
-    read_kernel<T, TYPE, G, wide><<<blocks, 256, 0, stream>>>(a);
-  else
-    read_kernel<T, TYPE, G, 1><<<blocks, 256, 0, stream>>>(a);
-  return launched();
+  return token_ranges(a.n, (int64_t)a.heads * G, 16, [&](int64_t from, int64_t n) {
+    ReadArgs r = a;
+    r.n = n;
+    r.k = (typename T::raw *)a.k + from * a.kt;
+    r.v = (typename T::raw *)a.v + from * a.vt;
+    r.slots = a.slots + from;
+    const int64_t rows = (n + 15) / 16 * 16 * a.heads;
+    const dim3 blocks((uint32_t)((rows + 256 / G - 1) / (256 / G)));
+    if (vec >= wide)
+      read_kernel<T, TYPE, G, wide><<<blocks, 256, 0, stream>>>(r);
+    else
+      read_kernel<T, TYPE, G, 1><<<blocks, 256, 0, stream>>>(r);
+  });
 }
 
 template <class T, int TYPE>

@@ -259,3 +259,22 @@ def test_rows_beside_one_another(kv):
         assert torch.equal(kv.attention(buf[:n, 0], *args, out=buf[:n, 0]), got)
 
 
+def test_more_rows_than_a_launch_has_threads_for(kv):
+    """2^19 tokens and a few of 2048 heads: 2^32 threads.  Most have no slot; the
+    first and last tokens, one row turned by their positions, are stored as by a
+    call of their own."""
+    n, heads, dim, page = (1 << 19) + 37, 2048, 64, 16
+    at = torch.tensor([0, 1, (1 << 19) - 2, (1 << 19) - 1, 1 << 19, n - 2, n - 1], device="cuda")
+    k, v = torch.randn(2, 1, heads, dim, generator=torch.Generator().manual_seed(2)).to(BF).cuda()
+    slots = torch.full((n,), -1, device="cuda")
+    slots[at] = torch.arange(7, device="cuda")
+    pos, table = torch.arange(n, device="cuda", dtype=torch.int32) % 1000, kv.rotary_table(1000, dim)
+    one, other = (kv.Cache.empty(1, page, heads, dim, I8) for _ in range(2))
+    kv.append(one, k.expand(n, -1, -1), v.expand(n, -1, -1), slots, positions=pos, table=table)
+    kv.append(other, k.expand(7, -1, -1), v.expand(7, -1, -1), slots[at], positions=pos[at],
+              table=table)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert torch.equal(getattr(one, name), getattr(other, name))
+    assert bool((one.k[:, :, :7].float().abs().amax(-1) == 127).all())
+
+

@@ -171,3 +171,14 @@ def test_workspace_of_loose_bounds():
     assert size(5, heads=64, tokens=640) == 128 * 32 * 10 * one
 
 
+def test_more_threads_than_a_launch_has():
+    """Batches whose workgroups have 2^32 threads or more are refused as such,
+    before anything is launched."""
+    cache = kv.CACHE.pack(FAKE, FAKE, 0, 0, 4, 16, 1, 64, kv.BF16)
+    for n_seq, tokens, max_q in ((1 << 24, 1 << 24, 1), (1 << 30, 1 << 30, 1),
+                                 (1 << 23, 1 << 20, 100)):
+        batch = kv.BATCH.pack(FAKE, 4, 4, FAKE, FAKE, n_seq, tokens, 1, 1.0, 1, 0, max_q, 64)
+        r = rows(FAKE, 64)
+        assert kv._lib().wait_kv_attention(cache, batch, r, r, None, None, 0, None) \
+            == B.WS_EUNSUPPORTED
+        assert b"workgroups" in kv._lib().wait_sim_last_error()
