@@ -89,7 +89,7 @@ __device__ __forceinline__ Range token_range(const Args &a, const Seq &s, int32_
   const int32_t p = s.m - s.n + i;
   r.hi = min(s.m, a.capacity);
   if (a.causal) r.hi = max(min(r.hi, p + 1), 0);
-  r.lo = a.window && p >= a.window ? p - a.window + 1 : 0;  // p may be negative
+  r.lo = a.window ? max(max(p, 0) - a.window + 1, 0) : 0;
   r.lo = min(r.lo, r.hi);
   return r;
 }
@@ -854,10 +854,9 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
       }
       if (keys && wave == 0 && lane < M::keys) {
         const bool next_edge = k1 < block_every.lo || k1 + M::keys > block_every.hi;
-        if (!(key_there >> lane & 1)) {  // loaded from another row
-          ks = vs = 0.0f;
-        } else if (next_edge && !isfinite(vs)) {
-          bad = true;
+        const bool there = key_there >> lane & 1;
+        if (!there | (next_edge & !isfinite(vs))) {
+          bad |= there;
           vs = 0.0f;
         }
         float *sc = (float *)(smem + 4 * M::side + ((t + 1) & 1) * M::scales);
