@@ -655,7 +655,7 @@ __device__ __forceinline__ void copy_to_lds(const char *from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :
                : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory", "m0");
+               : "memory");
 }
 __device__ __forceinline__ void await_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
