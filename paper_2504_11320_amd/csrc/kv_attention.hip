@@ -41,12 +41,14 @@ struct Args {
   int32_t causal, window;
   int32_t q_bf16;
   // results of parts, the sums o and (m, l): few rows [request][KV head]
-  // [few_room][part], many rows [token][head][part]
+  // [few_room][part] or [KV head][row of the batch][part], many rows
+  // [token][head][part]
   float *few_o, *many_o;
   float2 *few_ml, *many_ml;
   int32_t few_splits, few_chunk;    // of a few-rows launch: parts, keys a part
   int32_t few_blocks;               // row blocks of a request
   int32_t few_room;                 // rows of a request that may have parts
+  int32_t few_head, few_seq, few_token;  // slots from a KV head, request or token to the next
   int32_t many_splits, many_chunk;  // of a many-rows launch
   int32_t both;          // requests of more than 16 rows are the many-rows blocks'
   int32_t row_blocks;    // numbers of row blocks of the many-rows launch
@@ -121,6 +123,13 @@ __device__ __forceinline__ int32_t parts_of(Range r, int32_t chunk, int32_t spli
 // was laid out for has no room for parts.
 __device__ __forceinline__ int32_t few_parts(const Args &a, Range r, int32_t rows) {
   return rows > a.few_room ? 1 : parts_of(r, a.few_chunk, a.few_splits);
+}
+
+// The slot in the workspace of the first part of a few-rows row.
+__device__ __forceinline__ int64_t few_slot(const Args &a, const Seq &s, int32_t b, int32_t h,
+                                            int32_t row) {
+  return ((int64_t)h * a.few_head + (int64_t)b * a.few_seq + (int64_t)s.q0 * a.few_token + row) *
+         a.few_splits;
 }
 
 // Key j of a request, 0 < end: its page's entry in the table, read ahead (the
@@ -595,8 +604,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         for (int i = 0; i < 4; ++i) p[i] = out_bits(a, x[i] * inv);
         if (a.lse && d == 0) a.lse[q_row * a.heads + hd] = natural_lse(top, total);
       } else {
-        const int64_t to =
-            ((int64_t)(b * a.kv_heads + h) * a.few_room + r0 + r) * a.few_splits + split;
+        const int64_t to = few_slot(a, s, b, h, r0 + r) + split;
         *reinterpret_cast<f32x4 *>(a.few_o + to * D + d) = x;
         if (d == 0) a.few_ml[to] = make_float2(top, total);
       }
@@ -1194,13 +1202,12 @@ __device__ __forceinline__ void join_few(const Args &a, int32_t id, int32_t nth,
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
   if (rows == 0 || rows > a.few_room) return;
-  const int64_t from = (int64_t)(b * a.kv_heads + head / a.group) * a.few_room;
   for (int32_t i = nth; i < s.n; i += step) {
     const int32_t row = i * a.group + head % a.group, r0 = row / kFewRows * kFewRows;
     const int32_t parts =
         few_parts(a, block_range(a, s, r0, min(r0 + kFewRows, rows) - 1, 32), rows);
     if (parts == 1) continue;
-    const int64_t at = (from + row) * a.few_splits;
+    const int64_t at = few_slot(a, s, b, head / a.group, row);
     shared[mine][lane] = join_parts<D>(a.few_o + at * D, a.few_ml + at, mine, groups, parts);
     __syncthreads();
     if (mine == 0) {
@@ -1252,7 +1259,7 @@ __global__ void __launch_bounds__(256) join_kernel(Args a, int32_t few, int32_t 
 // How a batch is laid out over workgroups.
 struct Layout {
   bool many, wide;
-  int32_t few_splits, few_chunk, few_blocks, few_room, many_splits, many_chunk, row_blocks;
+  int32_t few_splits, few_chunk, few_blocks, few_room, few_head, few_seq, few_token, many_splits, many_chunk, row_blocks;
   int64_t few_slots, many_slots;  // results of parts in the workspace
   int64_t bytes;
 };
@@ -1310,7 +1317,12 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // over 4 heads 31 us with 512 and 25 with 256.  D = 256 has tiles of 32 keys.
   const int64_t least = (full >= 64 ? 512 : 256) / (c.dim == 256 ? 2 : 1);
   split_keys(many_keys, full, 256, least, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
-  if (L.few_splits > 1) L.few_slots = pairs * L.few_room * L.few_splits;
+  // room for the rows that the bounds allow, or for those that there are
+  const int64_t bound = pairs * L.few_room, rows = (int64_t)b.n_tokens * b.heads;
+  L.few_head = (int32_t)(rows < bound ? rows / c.kv_heads : L.few_room);
+  L.few_seq = (int32_t)(rows < bound ? 0 : (int64_t)c.kv_heads * L.few_room);
+  L.few_token = rows < bound ? group : 0;
+  if (L.few_splits > 1) L.few_slots = std::min(rows, bound) * L.few_splits;
   if (L.many && L.many_splits > 1)
     L.many_slots = (int64_t)b.n_tokens * b.heads * L.many_splits;
   L.bytes = (L.few_slots + L.many_slots) * (c.dim + 2) * 4;
@@ -1449,6 +1461,9 @@ int wait_kv_attention(const ws_kv_cache *cache, const ws_kv_batch *batch, const 
     a.few_chunk = L.few_chunk;
     a.few_blocks = L.few_blocks;
     a.few_room = L.few_room;
+    a.few_head = L.few_head;
+    a.few_seq = L.few_seq;
+    a.few_token = L.few_token;
     a.many_splits = L.many_splits;
     a.many_chunk = L.many_chunk;
     a.both = L.many;

@@ -182,3 +182,21 @@ def test_more_threads_than_a_launch_has():
         assert kv._lib().wait_kv_attention(cache, batch, r, r, None, None, 0, None) \
             == B.WS_EUNSUPPORTED
         assert b"workgroups" in kv._lib().wait_sim_last_error()
+
+
+def test_workspace_without_bounds():
+    """Where the lengths of the queries are not given, the parts of a batch's rows
+    take no more room than the rows that there are."""
+    cache = kv.CACHE.pack(FAKE, FAKE, FAKE, FAKE, 8192, 16, 32, 128, kv.INT8)
+    one = 32 * (128 + 2) * 4           # the parts of a row
+    for tokens, heads in ((128, 32), (128, 64), (140, 32)):
+        batch = kv.BATCH.pack(FAKE, 8192, 8192, FAKE, FAKE, 128, tokens, heads, 1.0, 1, 0, tokens,
+                              8192 * 16)
+        n = C.c_size_t()
+        assert kv._lib().wait_kv_attention_workspace_bytes(cache, batch, n) == B.WS_OK
+        # beside the parts of many rows, of which there are 256 at most
+        assert n.value <= tokens * heads * (one + 256 * (128 + 2) * 4)
+        batch = kv.BATCH.pack(FAKE, 8192, 8192, FAKE, FAKE, 128, tokens, heads, 1.0, 1, 0, 2,
+                              8192 * 16)
+        assert kv._lib().wait_kv_attention_workspace_bytes(cache, batch, n) == B.WS_OK
+        assert n.value == tokens * heads * one
