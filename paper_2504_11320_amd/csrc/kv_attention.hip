@@ -260,6 +260,11 @@ __device__ __forceinline__ float unbounded_value(const Args &a, int32_t row, int
 // 2^-13, a normal number in 16 bits.  Where all values seen have smaller scales
 // (zeros), each key adds up to 2^96 to l, and 2^30 of them stay finite.
 constexpr float kLeastLog = -96.0f;
+// A scale that is not finite leaves the reference alone: it is the outputs that
+// cannot be finite, not the log-sum.
+__device__ __forceinline__ float reference_log(float scale) {
+  return isfinite(scale) ? fmaxf(log2f(fabsf(scale)), kLeastLog) : kLeastLog;
+}
 
 // o / l in the output's type; a query that sees nothing has l = 0.
 __device__ __forceinline__ float safe_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
@@ -436,7 +441,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id, char *smem) 
         }
         if (lane < 32) {
           kscale[lane] = ks;
-          vlog[lane] = fmaxf(log2f(fabsf(vs)), kLeastLog);
+          vlog[lane] = reference_log(vs);
           vscale[lane] = vs;
         }
       }
@@ -869,7 +874,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
         }
         float *sc = (float *)(smem + 4 * M::side + ((t + 1) & 1) * M::scales);
         sc[lane] = ks;
-        sc[M::keys + lane] = fmaxf(log2f(fabsf(vs)), kLeastLog);
+        sc[M::keys + lane] = reference_log(vs);
         sc[2 * M::keys + lane] = vs;
       }
     } else {

@@ -6,6 +6,7 @@ import math
 import pytest
 import torch
 
+from kv_util import attend, within
 from test_gpu_kv_attention import check, make
 
 pytestmark = pytest.mark.gpu
@@ -276,5 +277,26 @@ def test_more_rows_than_a_launch_has_threads_for(kv):
     for name in ("k", "v", "k_scale", "v_scale"):
         assert torch.equal(getattr(one, name), getattr(other, name))
     assert bool((one.k[:, :, :7].float().abs().amax(-1) == 127).all())
+
+
+@pytest.mark.parametrize("ctype", [E4, I8])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_scales_that_are_not_finite(kv, ctype, value):
+    """A value's scale that is not finite, seen by every token: no output of its
+    KV head is finite, and the log-sums do not depend on it."""
+    for q, m in (([1, 3], [90, 200]), ([1, 100], [90, 300])):
+        s = make(kv, q, m, 4, 2, 128, 16, ctype, BF)
+        c = s["cache"]
+        args = s["q"], c, s["pages"], s["starts"], s["kv_lens"]
+        want, lse = kv.attention(*args, return_lse=True)
+        for b, j in ((0, 40), (1, 135)):
+            at = int(s["pages"][b, j // 16])
+            c.v_scale[at, 0, j % 16] = value
+            c.v[at, 0, j % 16] = torch.ones(128, device="cuda").to(ctype)
+        got, same = kv.attention(*args, return_lse=True)
+        assert bool((~torch.isfinite(got[:, :2])).all()) and torch.equal(got[:, 2:], want[:, 2:])
+        # the reference of the softmax may be another: both are off by their bound
+        _, L, _, ltol = attend(s["q"], c, s["pages"], s["starts"], s["kv_lens"])
+        within(same, L, ltol, f"log-sum beside a scale of {value}")
 
 
