@@ -116,7 +116,8 @@ typedef struct {
   int32_t causal;
   int32_t window;         /* 0: none */
   /* Upper bounds that the launch is laid out for.  Requests that are longer
-   * are computed all the same, only slower. */
+   * are computed all the same, only slower; bounds far above the lengths cost
+   * time and workspace. */
   int32_t max_q_len, max_kv_len;
 } ws_kv_batch;
 

@@ -5,8 +5,8 @@
 // both multiplied by 2^(m - m') whenever m grows to m'; the result is o / l.
 // Parts over different keys join the same way.  In an 8-bit cache with scales
 // s_j (keys) and t_j (values), z_j has s_j as a factor, and the weight of the
-// value's code is 2^(z_j - m) t_j: m runs over z_j + log2 t_j, which keeps these
-// weights within (0, 1], where the 16-bit floats are densest.
+// value's code is 2^(z_j - m) t_j: m runs over z_j + log2 |t_j|, which keeps these
+// weights within [-1, 1], where the 16-bit floats are densest.
 //
 // Matrix instructions compute S^T = K Q^T and O^T = V^T P^T.  S^T leaves a
 // query's scores in one lane column, four neighbouring keys in a lane, and that
@@ -283,7 +283,7 @@ __device__ __forceinline__ float natural_lse(float m, float l) {
 // the end; long requests are split over workgroups too.  Keys go from memory
 // into the matrix layout directly; values by way of shared memory, 32 rows a
 // wave, for the transposing read.  128 requests of 513 to 1512 keys, 32 heads of
-// 128: fp8 193 us (5.8 TB/s), bf16 371 us (5.8 TB/s), where a sum over 4 GiB
+// 128: fp8 193 us (5.8 TB/s), bf16 367 us (5.9 TB/s), where a sum over 4 GiB
 // reads 6.2 TB/s.
 
 template <int TYPE>
@@ -631,10 +631,9 @@ __global__ void __launch_bounds__(64 * W, D == 256 ? 1 : 2) few_rows_kernel(Args
 // SIMD, and they take turns: while the one multiplies, the other does its
 // softmax, with a barrier at each change, so that the matrix and the vector
 // units both have work.  (D = 256: four waves of 32 rows, for want of
-// registers.)  Prompts of 6011 and 8192 tokens, 32 heads of 128, causal: bf16 760
-// us (853 TFLOP/s; 1223 in a library product of 8192^3), fp8 961 us, where the
-// scales' products come on top; D = 64 532 us.  The products alone take 470 us of
-// the 760, with their reads from shared memory 630.
+// registers.)  Prompts of 6011 and 8192 tokens, 32 heads of 128, causal: bf16 750
+// us (864 TFLOP/s; 1412 in a library product of 8192^3), fp8 915 us, where the
+// scales' products come on top; D = 64 485 us, of half the products.
 
 // for the scheduler: kinds of instructions, and products whose operands are read
 // ahead
@@ -1249,8 +1248,8 @@ __device__ __forceinline__ void join_many(const Args &a, int32_t id, int32_t key
   put_joined<D>(a, join_parts<D>(a.many_o + at * D, a.many_ml + at, 0, 1, parts), token, head);
 }
 
-// Both in one launch: 64 heads with 32 parts each 4.8 us; 543 x 32 rows, most of
-// them with 3, 7.2 us (12 with a wave a row, whose waves come in two turns).
+// Both in one launch: 64 heads with 32 parts each 4.9 us; 543 x 32 rows, most of
+// them with 3, 7.4 us (12 with a wave a row, whose waves come in two turns).
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(Args a, int32_t few, int32_t step, int32_t keys) {
   if ((int32_t)blockIdx.x < few)
@@ -1297,8 +1296,8 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // Blocks of 16 rows read the keys again, out of a cache where they run at the
   // same time; up to four of them are quicker than one block of 256 rows over
   // many keys: 16 requests of 10 to 16 tokens, 4 heads a KV head, over 1000 to
-  // 2000 keys in fp8 39 us against 57, of 5 to 8 tokens 25 against 53.  Over few
-  // keys they are not: 32 prompts of 30 to 60 tokens 47 us against 33.
+  // 2000 keys in fp8 37 us against 62, of 5 to 8 tokens 24 against 57.  Over few
+  // keys they are not: 32 prompts of 30 to 60 tokens 45 us against 32.
   L.many = max_rows > 4 * kFewRows || (max_rows > kFewRows && max_kv < 16 * max_rows);
   L.few_blocks = L.many ? 1 : (int32_t)ceil_div(max_rows, kFewRows);
   L.few_room = L.many ? kFewRows : (int32_t)max_rows;
@@ -1318,8 +1317,8 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // workgroups that have rows: as many as the tokens fill
   const int64_t full = ceil_div((int64_t)b.n_tokens * group, many_rows) * c.kv_heads;
   // Joining costs by the rows, so many of them take longer parts: a prompt of 512
-  // over 32 heads 28 us with parts of 512 keys and 33 with 256; a prompt of 1024
-  // over 4 heads 31 us with 512 and 25 with 256.  D = 256 has tiles of 32 keys.
+  // over 32 heads 26 us with parts of 512 keys and 28 with 256; a prompt of 1024
+  // over 4 heads 29 us with 512 and 24 with 256.  D = 256 has tiles of 32 keys.
   const int64_t least = (full >= 64 ? 512 : 256) / (c.dim == 256 ? 2 : 1);
   split_keys(many_keys, full, 256, least, (int64_t)1 << 30, 64, &L.many_splits, &L.many_chunk);
   // room for the rows that the bounds allow, or for those that there are

@@ -1,9 +1,9 @@
 // The Python side of include/wait_kv.h in C++: argument checks and marshalling.
 // A serving step calls these a few times a layer.  With the checks in Python
 // and ctypes, they took longer than the kernels of small calls: the rotation of
-// one token's 32 heads of 128 took 6.3 us a call there, 4.5 here (2.1 on the
-// GPU), rows of 128 tokens written and read back 16.0 there, 10.1 here (7.6 on
-// the GPU), 630 tokens read 9.4 there, 5.9 here (4.8).  kv.py has the
+// one token's 32 heads of 128 took 6.3 us a call there, 4.4 here (1.7 on the
+// GPU), rows of 128 tokens written and read back 16.0 there, 9.5 here (6.6 on
+// the GPU), 630 tokens read 9.4 there, 5.6 here (4.6).  kv.py has the
 // documentation and gives the library's entry points as addresses (bind), so
 // that this module works with whichever build of it is loaded.
 #include <Python.h>

@@ -226,7 +226,9 @@ def attention(q: torch.Tensor, cache: Cache, pages: torch.Tensor, starts: torch.
 
     ``starts``, ``kv_lens`` and ``pages`` are int32 and stay on the device;
     ``max_q_len`` and ``max_kv_len`` bound the lengths for the launch's layout
-    (by default from the shapes) and longer requests are only slower.
+    (by default from the shapes).  Requests beyond them are computed all the
+    same, only slower; bounds far above the lengths cost time and workspace too,
+    so a caller that knows the lengths gives them.
     Returns out, or (out, lse [tokens, heads] fp32); rows of queries outside every
     request stay as they are in a given ``out``, and are undefined otherwise.
     ``out`` may be q, and must not overlap it otherwise.  ``workspace`` (a uint8
