@@ -21,7 +21,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SRC_NAMES = ("wait_sim_host.hip", "sim_wait.hip", "sim_fcfs.hip",
              "sim_nested.hip", "sim_nested_unit.hip", "sim_wait_tv.hip", "sim_fcfs_tv.hip",
-             "sim_nested_tv.hip", "sim_fcfs_dist.hip", "kv_rows.hip", "kv_attention.hip")
+             "sim_nested_tv.hip", "sim_fcfs_dist.hip", "kv_rows.hip", "kv_attention.hip",
+             "kv_norm.hip", "kv_weigh.hip", "kv_evict.hip")
 SRCS = [os.path.join(CSRC, f) for f in SRC_NAMES]
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libwait_sim.so")

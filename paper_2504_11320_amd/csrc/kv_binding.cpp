@@ -1,4 +1,5 @@
-// The Python side of include/wait_kv.h in C++: argument checks and marshalling.
+// The Python side of include/wait_kv.h, wait_kv_norm.h and wait_kv_budget.h in
+// C++: argument checks and marshalling.
 // A serving step calls these a few times a layer.  With the checks in Python
 // and ctypes, they took longer than the kernels of small calls: the rotation of
 // one token's 32 heads of 128 took 6.3 us a call there, 4.4 here (1.7 on the
@@ -21,7 +22,8 @@
 #include <cstring>
 #include <exception>
 
-#include "wait_kv.h"
+#include "wait_kv_budget.h"
+#include "wait_kv_norm.h"
 
 namespace {
 
@@ -30,6 +32,11 @@ decltype(&wait_kv_append) f_append;
 decltype(&wait_kv_read) f_read;
 decltype(&wait_kv_attention_workspace_bytes) f_workspace;
 decltype(&wait_kv_attention) f_attention;
+decltype(&wait_kv_norm_rotary) f_norm_rotary;
+decltype(&wait_kv_enter) f_enter;
+decltype(&wait_kv_weigh_workspace_bytes) f_weigh_workspace;
+decltype(&wait_kv_weigh) f_weigh;
+decltype(&wait_kv_evict) f_evict;
 PyObject *g_check, *g_stream, *g_device, *g_on;  // of binding.py and torch
 
 // Raised in Python as ValueError; Python's own errors as they are.
@@ -375,7 +382,7 @@ PyObject *read(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
 // The batch and its workspace's bytes.
 ws_kv_batch batch_of(const ws_kv_cache &c, int index, const at::Tensor &q, PyObject *const *v,
                      PyObject *max_q, PyObject *max_kv, PyObject *scale, bool causal,
-                     PyObject *window, size_t *bytes) {
+                     PyObject *window, decltype(f_workspace) workspace, size_t *bytes) {
   const at::Tensor &pages = tensor(v[0], "pages"), &starts = tensor(v[1], "starts"),
                    &lens = tensor(v[2], "kv_lens");
   need(q.dim() == 3, "q must be [tokens, heads, dim]");
@@ -415,7 +422,7 @@ ws_kv_batch batch_of(const ws_kv_cache &c, int index, const at::Tensor &q, PyObj
   b.window = (int32_t)std::max<int64_t>(std::min<int64_t>(whole(window), INT32_MAX), -1);
   b.max_q_len = (int32_t)std::max<int64_t>(bound(max_q, tokens), -1);
   b.max_kv_len = (int32_t)std::max<int64_t>(bound(max_kv, capacity), -1);
-  check(f_workspace(&c, &b, bytes));
+  check(workspace(&c, &b, bytes));
   return b;
 }
 
@@ -426,7 +433,8 @@ PyObject *attention_workspace_bytes(PyObject *, PyObject *const *v, Py_ssize_t n
     const ws_kv_cache c = cache_of(v[0]);
     const int index = (int)whole(v[1]);
     size_t bytes = 0;
-    batch_of(c, index, tensor(v[2], "q"), v + 3, v[6], v[7], Py_None, true, v[8], &bytes);
+    batch_of(c, index, tensor(v[2], "q"), v + 3, v[6], v[7], Py_None, true, v[8], f_workspace,
+             &bytes);
     return PyLong_FromSize_t(bytes);
   });
 }
@@ -444,7 +452,8 @@ PyObject *attention(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
     need(c.type == WS_KV_FP8 || c.type == WS_KV_INT8 || c.type == qr.type,
          "q must have the type of a 16-bit cache");
     size_t bytes = 0;
-    const ws_kv_batch b = batch_of(c, index, q, v + 3, v[6], v[7], v[8], truth(v[9]), v[10], &bytes);
+    const ws_kv_batch b = batch_of(c, index, q, v + 3, v[6], v[7], v[8], truth(v[9]), v[10],
+                                   f_workspace, &bytes);
     const bool want_lse = truth(v[11]);
     at::Tensor out, lse, space;
     if (v[12] == Py_None) {
@@ -491,12 +500,252 @@ PyObject *attention(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
   });
 }
 
-// bind(addresses of the five entry points, binding._check, stream of a GPU, current GPU,
+// A norm's weights, [dim] or [heads, dim]; ones where there are none.
+ws_kv_norm norm_of(const at::Tensor *w, PyObject *eps, const char *name, int64_t heads, int64_t dim,
+                   int index) {
+  ws_kv_norm n{};
+  n.type = WS_KV_FP32;
+  n.eps = (float)PyFloat_AsDouble(eps);
+  if (PyErr_Occurred()) throw Refused();
+  if (!w) return n;
+  no_gradient(*w, name);
+  n.type = kv_type(w->scalar_type());
+  if (!wide(n.type)) refuse("%s must be bf16, fp16 or fp32", name);
+  const bool each = w->dim() == 2;
+  if (!(each || w->dim() == 1) || w->size(-1) != dim || (each && w->size(0) != heads))
+    refuse("%s must be [dim] or [heads, dim]", name);
+  if (w->stride(-1) != 1 && dim > 1) refuse("%s: a head's weights must be contiguous", name);
+  if (index_of(*w) != index) refuse("%s must be on the same device", name);
+  n.weight = w->data_ptr();
+  n.head_stride = each ? w->stride(0) : 0;
+  return n;
+}
+
+// norm_rotary(x, weight or None, positions or None, table or None, eps, interleaved, out or None)
+PyObject *norm_rotary(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+  ARGS(7)
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &x = tensor(v[0], "x");
+    const int index = index_of(x);
+    const ws_kv_rows xr = rows(x, "x", index);
+    const int64_t n = x.size(0), heads = x.size(1), dim = x.size(2);
+    need(heads <= INT32_MAX && dim <= INT32_MAX, "x is too large");
+    const ws_kv_norm w = norm_of(tensor_or_none(v[1], "weight"), v[4], "weight", heads, dim, index);
+    ws_kv_turn t;
+    const bool turned = v[2] != Py_None || v[3] != Py_None;
+    if (turned)
+      t = turn(tensor_or_none(v[2], "positions"), tensor_or_none(v[3], "table"), n, dim, truth(v[5]),
+               index);
+    at::Tensor out;
+    if (v[6] == Py_None) {
+      need(index >= 0, "the operators run on the GPU");
+      out = at::empty_like(x);
+    } else {
+      out = tensor(v[6], "out");
+      need(out.sizes() == x.sizes() && out.scalar_type() == x.scalar_type(),
+           "out must have x's shape and type");
+      apart(out, "out");
+    }
+    const ws_kv_rows o = rows(out, "out", index);
+    if (n && heads)
+      run(index, [&](void *s) {
+        return f_norm_rotary(&xr, &o, n, (int32_t)heads, (int32_t)dim, &w, turned ? &t : nullptr, s);
+      });
+    if (v[6] != Py_None) {
+      written(out);
+      Py_INCREF(v[6]);
+      return v[6];
+    }
+    return THPVariable_Wrap(std::move(out));
+  });
+}
+
+// enter(cache bytes, GPU, the cache's tensors, q, k, v, slots, positions or None, table or None,
+//       q_norm or None, k_norm or None, eps, interleaved, out or None): the queries
+PyObject *enter(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+  ARGS(14)
+  return guarded([&]() -> PyObject * {
+    const ws_kv_cache c = cache_of(v[0]);
+    const int index = (int)whole(v[1]);
+    need(PyTuple_Check(v[2]), "not a cache");
+    const at::Tensor &q = tensor(v[3], "q"), &k = tensor(v[4], "k"), &w = tensor(v[5], "v"),
+                     &slots = tensor(v[6], "slots");
+    const ws_kv_rows qr = rows(q, "q", index), kr = rows(k, "k", index), wr = rows(w, "v", index);
+    const int64_t n = slots_of(slots, index), heads = q.size(1);
+    need(k.size(0) == n && k.size(1) == c.kv_heads && k.size(2) == c.dim && k.sizes() == w.sizes() &&
+             kr.type == wr.type,
+         "k and v must be [slots, kv_heads, dim] of one type");
+    need(q.size(0) == n && heads >= 1 && heads <= INT32_MAX && q.size(2) == c.dim &&
+             qr.type == kr.type,
+         "q must be [slots, heads, dim] of the type of k and v");
+    ws_kv_turn t;
+    const bool turned = v[7] != Py_None || v[8] != Py_None;
+    if (turned)
+      t = turn(tensor_or_none(v[7], "positions"), tensor_or_none(v[8], "table"), n, c.dim,
+               truth(v[12]), index);
+    const at::Tensor *qw = tensor_or_none(v[9], "q_norm"), *kw = tensor_or_none(v[10], "k_norm");
+    const ws_kv_norm qn = norm_of(qw, v[11], "q_norm", heads, c.dim, index),
+                     kn = norm_of(kw, v[11], "k_norm", c.kv_heads, c.dim, index);
+    at::Tensor out;
+    if (v[13] == Py_None) {
+      need(index >= 0, "the operators run on the GPU");
+      out = at::empty(q.sizes(), q.options());
+    } else {
+      out = tensor(v[13], "out");
+      need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(),
+           "out must have q's shape and type");
+      apart(out, "out");
+    }
+    const ws_kv_rows o = rows(out, "out", index);
+    run(index, [&](void *s) {
+      return f_enter(&c, &qr, &o, (int32_t)heads, &kr, &wr, slots.data_ptr<int64_t>(), n,
+                     qw ? &qn : nullptr, kw ? &kn : nullptr, turned ? &t : nullptr, s);
+    });
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(v[2]); ++i)
+      if (auto *t = tensor_or_none(PyTuple_GET_ITEM(v[2], i), "the cache's")) written(*t);
+    if (v[13] != Py_None) {
+      written(out);
+      Py_INCREF(v[13]);
+      return v[13];
+    }
+    return THPVariable_Wrap(std::move(out));
+  });
+}
+
+// Accumulated weights of the cache's rows.
+const at::Tensor &weights_of(PyObject *o, const ws_kv_cache &c, int index) {
+  const at::Tensor &t = tensor(o, "weights");
+  no_gradient(t, "weights");
+  need(t.dim() == 3 && t.size(0) == c.pages && t.size(1) == c.kv_heads && t.size(2) == c.page_size &&
+           t.scalar_type() == at::kFloat && t.is_contiguous() && index_of(t) == index,
+       "weights must be [pages, kv_heads, page_size], fp32, contiguous, on the cache's device");
+  return t;
+}
+
+// weigh_workspace_bytes(cache bytes, GPU, q, pages, starts, kv_lens, max_q, max_kv, causal, window)
+PyObject *weigh_workspace_bytes(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+  ARGS(10)
+  return guarded([&]() -> PyObject * {
+    const ws_kv_cache c = cache_of(v[0]);
+    const int index = (int)whole(v[1]);
+    size_t bytes = 0;
+    batch_of(c, index, tensor(v[2], "q"), v + 3, v[6], v[7], Py_None, truth(v[8]), v[9],
+             f_weigh_workspace, &bytes);
+    return PyLong_FromSize_t(bytes);
+  });
+}
+
+// weigh(cache bytes, GPU, q, pages, starts, kv_lens, max_q, max_kv, scale, causal, window, lse,
+//       weights, accumulate, workspace or None)
+PyObject *weigh(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+  ARGS(15)
+  return guarded([&]() -> PyObject * {
+    const ws_kv_cache c = cache_of(v[0]);
+    const int index = (int)whole(v[1]);
+    const at::Tensor &q = tensor(v[2], "q"), &lse = tensor(v[11], "lse");
+    const ws_kv_rows qr = rows(q, "q", index);
+    need(qr.type != WS_KV_FP32, "q must be bf16 or fp16");
+    need(c.type == WS_KV_FP8 || c.type == WS_KV_INT8 || c.type == qr.type,
+         "q must have the type of a 16-bit cache");
+    no_gradient(lse, "lse");
+    need(lse.dim() == 2 && lse.size(0) == q.size(0) && lse.size(1) == q.size(1) &&
+             lse.scalar_type() == at::kFloat && lse.is_contiguous() && index_of(lse) == index,
+         "lse must be [tokens, heads], fp32, contiguous, on the cache's device");
+    const at::Tensor &weights = weights_of(v[12], c, index);
+    size_t bytes = 0;
+    const ws_kv_batch b = batch_of(c, index, q, v + 3, v[6], v[7], v[8], truth(v[9]), v[10],
+                                   f_weigh_workspace, &bytes);
+    const bool accumulate = truth(v[13]);
+    at::Tensor space;
+    void *ptr = nullptr;
+    size_t have = 0;
+    if (v[14] != Py_None) {
+      const at::Tensor &t = tensor(v[14], "workspace");
+      need(t.is_contiguous() && index_of(t) == index,
+           "workspace must be contiguous, on the cache's device");
+      ptr = t.data_ptr();
+      have = t.nbytes();
+    } else if (bytes) {
+      need(index >= 0, "the operators run on the GPU");
+      space = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
+      ptr = space.data_ptr();
+      have = bytes;
+    }
+    run(index, [&](void *s) {
+      return f_weigh(&c, &b, &qr, lse.data_ptr<float>(), weights.data_ptr<float>(), accumulate, ptr,
+                     have, s);
+    });
+    if (v[14] != Py_None) written(tensor(v[14], "workspace"));
+    written(weights);
+    Py_RETURN_NONE;
+  });
+}
+
+// evict(cache bytes, GPU, the cache's tensors, pages, kv_lens, weights, keep, recent, to or None,
+//       max_kv or None): (kept, new lengths)
+PyObject *evict(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+  ARGS(10)
+  return guarded([&]() -> PyObject * {
+    const ws_kv_cache c = cache_of(v[0]);
+    const int index = (int)whole(v[1]);
+    need(PyTuple_Check(v[2]), "not a cache");
+    const at::Tensor &pages = tensor(v[3], "pages"), &lens = tensor(v[4], "kv_lens");
+    const at::Tensor *to = tensor_or_none(v[8], "to");
+    for (const at::Tensor *t : {&pages, to})
+      if (t && !(t->dim() == 2 && t->scalar_type() == at::kInt && t->size(0) == pages.size(0) &&
+                 (t->size(1) <= 1 || t->stride(1) == 1) && index_of(*t) == index))
+        refuse("%s must be [requests, pages], int32, rows contiguous, on the cache's device",
+               t == to ? "to" : "pages");
+    const int64_t n_seq = pages.size(0), keep = whole(v[6]), recent = whole(v[7]);
+    need(lens.dim() == 1 && lens.size(0) == n_seq && lens.scalar_type() == at::kInt &&
+             lens.is_contiguous() && index_of(lens) == index,
+         "kv_lens must be one int32 a request, contiguous, on the cache's device");
+    need(n_seq <= INT32_MAX && pages.size(1) <= INT32_MAX && (!to || to->size(1) <= INT32_MAX),
+         "the batch is too large");
+    need(keep >= 1 && keep <= INT32_MAX, "at least one key must be kept, and fewer than 2^31");
+    need(recent >= 0 && recent <= keep, "recent must be 0 to keep");
+    const at::Tensor &weights = weights_of(v[5], c, index);
+    const int64_t capacity = std::min<int64_t>(pages.size(1) * c.page_size, INT32_MAX);
+    ws_kv_eviction e{};
+    e.table = pages.data_ptr<int32_t>();
+    e.table_stride = n_seq > 1 ? pages.stride(0) : pages.size(1);
+    e.table_cols = (int32_t)pages.size(1);
+    e.kv_lens = lens.data_ptr<int32_t>();
+    e.n_seq = (int32_t)n_seq;
+    e.keep = (int32_t)keep;
+    e.recent = (int32_t)recent;
+    if (to) {
+      need(to->size(1) * c.page_size >= keep, "to must have pages for the kept rows");
+      e.to = to->data_ptr<int32_t>();
+      e.to_stride = n_seq > 1 ? to->stride(0) : to->size(1);
+      e.to_cols = (int32_t)to->size(1);
+    }
+    const int64_t bound = v[9] == Py_None ? capacity : std::min<int64_t>(whole(v[9]), capacity);
+    e.max_kv_len = (int32_t)std::max<int64_t>(bound, -1);
+    need(index >= 0, "the operators run on the GPU");
+    at::Tensor kept = at::empty({n_seq, c.kv_heads, keep}, pages.options()),
+               left = at::empty({n_seq}, lens.options());
+    run(index, [&](void *s) {
+      return f_evict(&c, &e, weights.data_ptr<float>(), kept.data_ptr<int32_t>(),
+                     left.data_ptr<int32_t>(), s);
+    });
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(v[2]); ++i)
+      if (auto *t = tensor_or_none(PyTuple_GET_ITEM(v[2], i), "the cache's")) written(*t);
+    written(weights);
+    PyObject *a = THPVariable_Wrap(std::move(kept)), *z = a ? THPVariable_Wrap(std::move(left)) : nullptr;
+    PyObject *both = z ? PyTuple_Pack(2, a, z) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(z);
+    return both;
+  });
+}
+
+// bind(addresses of the ten entry points, binding._check, stream of a GPU, current GPU,
 //      torch.cuda.device)
 PyObject *bind(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
-  ARGS(9)
-  void *p[5];
-  for (int i = 0; i < 5; ++i) {
+  ARGS(14)
+  void *p[10];
+  for (int i = 0; i < 10; ++i) {
     p[i] = PyLong_AsVoidPtr(v[i]);
     if (PyErr_Occurred()) return nullptr;
   }
@@ -505,10 +754,15 @@ PyObject *bind(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
   f_read = reinterpret_cast<decltype(f_read)>(p[2]);
   f_workspace = reinterpret_cast<decltype(f_workspace)>(p[3]);
   f_attention = reinterpret_cast<decltype(f_attention)>(p[4]);
+  f_norm_rotary = reinterpret_cast<decltype(f_norm_rotary)>(p[5]);
+  f_enter = reinterpret_cast<decltype(f_enter)>(p[6]);
+  f_weigh_workspace = reinterpret_cast<decltype(f_weigh_workspace)>(p[7]);
+  f_weigh = reinterpret_cast<decltype(f_weigh)>(p[8]);
+  f_evict = reinterpret_cast<decltype(f_evict)>(p[9]);
   PyObject **kept[4] = {&g_check, &g_stream, &g_device, &g_on};
   for (int i = 0; i < 4; ++i) {
-    Py_INCREF(v[5 + i]);
-    Py_XSETREF(*kept[i], v[5 + i]);
+    Py_INCREF(v[10 + i]);
+    Py_XSETREF(*kept[i], v[10 + i]);
   }
   Py_RETURN_NONE;
 }
@@ -516,7 +770,9 @@ PyObject *bind(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),      METHOD(rotary),    METHOD(cache),
                          METHOD(append),    METHOD(read),      METHOD(attention_workspace_bytes),
-                         METHOD(attention), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(attention), METHOD(norm_rotary), METHOD(enter),
+                         METHOD(weigh_workspace_bytes), METHOD(weigh), METHOD(evict),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv", "Argument checks of kv.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

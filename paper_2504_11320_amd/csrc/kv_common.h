@@ -58,23 +58,24 @@ inline int check_rows(const ws_kv_rows *r, int64_t n, const char *null_msg) {
   return WS_OK;
 }
 
-// Whether vectors of a share memory with vectors of b: n tokens of `heads` of
-// dim elements of one size each.  Exact where the token strides are the same, as
-// of parts of one buffer's rows; others share it if their ranges meet.
-inline bool overlap(const ws_kv_rows &a, const ws_kv_rows &b, int64_t n, int64_t heads, int64_t dim) {
+// Whether vectors of a share memory with vectors of b: n tokens of heads_a and
+// heads_b of dim elements of one size each.  Exact where the token strides are the
+// same, as of parts of one buffer's rows; others share it if their ranges meet.
+inline bool overlap(const ws_kv_rows &a, const ws_kv_rows &b, int64_t n, int64_t heads_a,
+                    int64_t heads_b, int64_t dim) {
   using wide = __int128;
-  if (n < 1 || heads < 1 || dim < 1) return false;
+  if (n < 1 || heads_a < 1 || heads_b < 1 || dim < 1) return false;
   const wide e = type_bytes(a.type), len = dim * e;
   struct Span {
     wide at, lo, hi;
   };
-  auto span = [&](const ws_kv_rows &r) {
+  auto span = [&](const ws_kv_rows &r, int64_t heads) {
     const wide tokens = (wide)(n - 1) * r.token_stride * e, step = (wide)(heads - 1) * r.head_stride * e;
     const wide at = (wide)(uintptr_t)r.data, none = 0;
     return Span{at, at + (tokens < 0 ? tokens : none) + (step < 0 ? step : none),
                 at + (tokens > 0 ? tokens : none) + (step > 0 ? step : none) + len};
   };
-  const Span x = span(a), y = span(b);
+  const Span x = span(a, heads_a), y = span(b, heads_b);
   if (x.hi <= y.lo || y.hi <= x.lo) return false;
   if (n > 1 && a.token_stride != b.token_stride) return true;
   // heads i of a and j of b are `apart` bytes apart at one token, and by a
@@ -90,12 +91,15 @@ inline bool overlap(const ws_kv_rows &a, const ws_kv_rows &b, int64_t n, int64_t
     return false;
   };
   const bool same = a.head_stride == b.head_stride;
-  for (int64_t i = 0; i < heads; ++i)
-    for (int64_t j = 0; j < heads; ++j) {
+  for (int64_t i = 0; i < heads_a; ++i)
+    for (int64_t j = 0; j < heads_b; ++j) {
       if (same && i && j) break;  // differences of heads, each once
       if (meet(y.at - x.at + ((wide)j * b.head_stride - (wide)i * a.head_stride) * e)) return true;
     }
   return false;
+}
+inline bool overlap(const ws_kv_rows &a, const ws_kv_rows &b, int64_t n, int64_t heads, int64_t dim) {
+  return overlap(a, b, n, heads, heads, dim);
 }
 inline bool one_place(const ws_kv_rows &a, const ws_kv_rows &b) {
   return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;

@@ -1,12 +1,17 @@
 """The KV path of one serving iteration on the card: Python side of
-include/wait_kv.h (the argument checks are in csrc/kv_binding.cpp; PyTorch
-allocates buffers and supplies the stream).
+include/wait_kv.h, wait_kv_norm.h and wait_kv_budget.h (the argument checks are in
+csrc/kv_binding.cpp; PyTorch allocates buffers and supplies the stream).
 
 * ``rotary_table`` / ``rotary``: vectors turned by their positions.
 * ``Cache``: one layer's paged cache, in 16 bits or quantised to 8.
 * ``append``: new keys and values into the cache, the keys turned on the way.
 * ``read``: rows of the cache back as values.
 * ``attention``: every token's attention over its request's pages.
+* ``norm_rotary``: vectors normed, then turned.
+* ``enter``: a batch's queries, keys and values into a layer: ``norm_rotary`` of
+  the queries and ``append`` of the keys and values, the keys normed, at once.
+* ``weigh`` / ``evict``: the attention that every cached key received, and the
+  way back to a budget of keys a request by it.
 
 Every function runs asynchronously on the current stream of its tensors'
 device and needs the HIP library: there is no fallback.  Results carry no
@@ -38,6 +43,8 @@ ROWS = struct.Struct("Pqqi4x")              # ws_kv_rows
 TURN = struct.Struct("PPiiii")              # ws_kv_turn
 CACHE = struct.Struct("PPPPiiiii4x")        # ws_kv_cache
 BATCH = struct.Struct("Pqi4xPPiiifiiii")    # ws_kv_batch
+NORM = struct.Struct("Pqif")                # ws_kv_norm
+EVICTION = struct.Struct("Pqi4xPiii4xPqii")  # ws_kv_eviction
 
 _fn = _kv = None
 
@@ -52,6 +59,11 @@ def _lib():
         L.wait_kv_read.argtypes = [s, p, i64, s, s, p]
         L.wait_kv_attention_workspace_bytes.argtypes = [s, s, C.POINTER(C.c_size_t)]
         L.wait_kv_attention.argtypes = [s, s, s, s, p, p, C.c_size_t, p]
+        L.wait_kv_norm_rotary.argtypes = [s, s, i64, i32, i32, s, s, p]
+        L.wait_kv_enter.argtypes = [s, s, s, i32, s, s, p, i64, s, s, s, p]
+        L.wait_kv_weigh_workspace_bytes.argtypes = [s, s, C.POINTER(C.c_size_t)]
+        L.wait_kv_weigh.argtypes = [s, s, s, p, p, i32, p, C.c_size_t, p]
+        L.wait_kv_evict.argtypes = [s, s, p, p, p, p]
         _fn = L
     return _fn
 
@@ -70,7 +82,8 @@ def _native():
         current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         native.bind(*(C.cast(f, C.c_void_p).value for f in (
             L.wait_kv_rotary, L.wait_kv_append, L.wait_kv_read,
-            L.wait_kv_attention_workspace_bytes, L.wait_kv_attention)),
+            L.wait_kv_attention_workspace_bytes, L.wait_kv_attention, L.wait_kv_norm_rotary,
+            L.wait_kv_enter, L.wait_kv_weigh_workspace_bytes, L.wait_kv_weigh, L.wait_kv_evict)),
             B._check, stream, current, torch.cuda.device)
         _kv = native
     return _kv
@@ -133,6 +146,19 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *,
     gradient's way through a rotation.  ``out`` may be x, and must not overlap
     it otherwise.  A position outside the table gives NaN."""
     return _native().rotary(x, positions, table, interleaved, inverse, out)
+
+
+def norm_rotary(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None, *,
+                eps: float = 1e-6, interleaved: bool = False,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [tokens, heads, dim] with every vector over its root mean square,
+    x / sqrt(mean(x^2) + eps), times ``weight`` ([dim], or [heads, dim] where each
+    head has its own; None: ones), then turned as by ``rotary`` where ``positions``
+    and ``table`` are given.  In 32 bits, rounded once at the end, whatever the
+    types of x and the weights (bf16, fp16 or fp32).  ``out`` may be x, and must
+    not overlap it otherwise."""
+    return _native().norm_rotary(x, weight, positions, table, eps, interleaved, out)
 
 
 # ------------------------------------------------------------------ cache ----
@@ -199,6 +225,23 @@ def append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
                      cache._tensors)
 
 
+def enter(cache: Cache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *,
+          positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+          q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+          eps: float = 1e-6, interleaved: bool = False,
+          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A batch's q [tokens, heads, dim], k and v [tokens, kv_heads, dim] into a
+    layer, in one pass: returns the queries normed by ``q_norm`` and turned, and
+    appends the keys, normed by ``k_norm`` and turned, and the values to the
+    cache (``append``).  Norms are those of ``norm_rotary``; without weights for
+    it a side is not normed, without ``positions`` and ``table`` neither is
+    turned.  A token without a slot gives its queries all the same.  ``out`` may
+    be q, which may lie beside k and v in the rows of one product, and must not
+    overlap q otherwise, nor k or v."""
+    return _native().enter(cache._c, cache._index, cache._tensors, q, k, v, slots, positions, table,
+                           q_norm, k_norm, eps, interleaved, out)
+
+
 def read(cache: Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
          out: Optional[tuple] = None) -> tuple:
     """(k, v) [slots, kv_heads, dim] of the cache's slots, as values rounded
@@ -245,3 +288,58 @@ def attention_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor
     """Bytes that ``attention`` takes as its workspace for these shapes."""
     return _native().attention_workspace_bytes(cache._c, cache._index, q, pages, starts, kv_lens,
                                                max_q_len, max_kv_len, window)
+
+
+# ----------------------------------------------------------------- budget ----
+
+
+def weigh(q: torch.Tensor, lse: torch.Tensor, cache: Cache, pages: torch.Tensor,
+          starts: torch.Tensor, kv_lens: torch.Tensor, weights: torch.Tensor, *,
+          max_q_len: Optional[int] = None, max_kv_len: Optional[int] = None,
+          scale: Optional[float] = None, causal: bool = True, window: int = 0,
+          accumulate: bool = True, workspace: Optional[torch.Tensor] = None) -> None:
+    """Adds to ``weights`` [pages, kv_heads, page_size] (fp32, one for each row of
+    the cache) the attention that each key received from the batch: the sum of
+    its softmax weights over the tokens that see it and the heads that read it.
+    The batch, its bounds, mask and scale are those that ``attention`` was called
+    with, and ``lse`` the log-sums that it returned.
+
+    The keys of the batch's own tokens, the last starts[b + 1] - starts[b] of
+    request b, are new and start from zero, whatever their rows held; without
+    ``accumulate`` all keys of the batch's requests do (so that the last tokens of
+    a prompt alone can say which of its keys matter).  Keys of other requests stay
+    as they are.  Requests must not share pages.  ``workspace`` (a uint8 tensor of
+    ``weigh_workspace_bytes``) is taken from PyTorch where it is not given."""
+    _native().weigh(cache._c, cache._index, q, pages, starts, kv_lens, max_q_len, max_kv_len, scale,
+                    causal, window, lse, weights, accumulate, workspace)
+
+
+def weigh_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor, starts: torch.Tensor,
+                          kv_lens: torch.Tensor, *, max_q_len: Optional[int] = None,
+                          max_kv_len: Optional[int] = None, causal: bool = True,
+                          window: int = 0) -> int:
+    """Bytes that ``weigh`` takes as its workspace for these shapes."""
+    return _native().weigh_workspace_bytes(cache._c, cache._index, q, pages, starts, kv_lens,
+                                           max_q_len, max_kv_len, causal, window)
+
+
+def evict(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, weights: torch.Tensor, *,
+          keep: int, recent: int = 0, to: Optional[torch.Tensor] = None,
+          max_kv_len: Optional[int] = None) -> tuple:
+    """Takes every request back to ``keep`` keys: of one that has more, each KV
+    head keeps the last ``recent`` and, of the others, those with the largest
+    ``weights`` (equal ones: the lower index; NaN is larger than all else).  Kept
+    rows, their scales and their weights move, in their order, to the front of
+    the request's pages, or to those of ``to`` [requests, pages for keep keys],
+    which are no request's, and ``pages`` can then be given back.  Rows behind
+    the kept ones stay as they are; pages of ``pages`` behind them are free.
+
+    ``pages``, ``to`` and ``kv_lens`` are int32 and stay on the device;
+    ``max_kv_len`` bounds the lengths for the launch's layout.  Requests share no
+    pages, and all of their pages are there (include/wait_kv_budget.h).  Returns
+    (kept [requests, kv_heads, keep] int32, the indices of the kept keys, -1
+    behind a request's last; new lengths [requests], min(kv_lens, keep)).  Attention over the
+    kept rows must not be windowed by positions: their indices are new ones, and
+    differ from head to head."""
+    return _native().evict(cache._c, cache._index, cache._tensors, pages, kv_lens, weights, keep,
+                           recent, to, max_kv_len)

@@ -1,0 +1,276 @@
+"""Norms, accumulated weights and eviction without a GPU: exports, structs,
+refusals of the C ABI and of the Python side."""
+import os
+import re
+
+import pytest
+import torch
+
+from kv_more_util import kept_keys
+from paper_2504_11320_amd import binding as B
+from paper_2504_11320_amd import kv
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE = 1 << 40   # never dereferenced: the checks come first
+
+
+@pytest.mark.parametrize("header,names", [
+    ("wait_kv_norm.h", ["wait_kv_enter", "wait_kv_norm_rotary"]),
+    ("wait_kv_budget.h", ["wait_kv_evict", "wait_kv_weigh", "wait_kv_weigh_workspace_bytes"])])
+def test_library_exports_header_symbols(header, names):
+    src = open(os.path.join(ROOT, "include", header)).read()
+    assert sorted(set(re.findall(r"^int (wait_kv_\w+)\s*\(", src, re.M))) == names
+    for n in names:
+        assert hasattr(B.lib(), n), n
+
+
+def cache(**kw):
+    d = dict(k=FAKE, v=FAKE << 1, k_scale=0, v_scale=0, pages=4, page_size=16, kv_heads=2, dim=64,
+             type=kv.BF16)
+    d.update(kw)
+    return kv.CACHE.pack(*d.values())
+
+
+def rows(data=FAKE << 2, token=128, head=64, type=kv.BF16):
+    return kv.ROWS.pack(data, token, head, type)
+
+
+def turn(**kw):
+    d = dict(table=FAKE, positions=FAKE, positions_32=0, n_table=10, part=32, interleaved=0)
+    d.update(kw)
+    return kv.TURN.pack(*d.values())
+
+
+def norm(weight=FAKE, stride=0, type=kv.BF16, eps=1e-6):
+    return kv.NORM.pack(weight, stride, type, eps)
+
+
+def refused(rc, code=None):
+    assert rc == (B.WS_EINVAL if code is None else code), rc
+
+
+def test_norm_rotary_refusals():
+    L = kv._lib()
+
+    def call(x=None, out=None, n=3, heads=2, dim=64, w=norm(), t=None):
+        return L.wait_kv_norm_rotary(x or rows(), out or x or rows(), n, heads, dim, w, t, None)
+
+    for kw in (dict(n=-1), dict(heads=0), dict(dim=0), dict(dim=65537), dict(x=rows(data=0)),
+               dict(x=rows(type=kv.FP8)), dict(x=rows(data=(FAKE << 2) + 1)),
+               dict(out=rows(type=kv.FP16)), dict(w=norm(type=kv.INT8)),
+               dict(w=norm(weight=FAKE + 1)), dict(w=norm(type=kv.FP32, weight=FAKE + 2)),
+               dict(w=norm(eps=-1e-6)), dict(w=norm(eps=float("nan"))),
+               dict(w=norm(eps=float("inf"))), dict(t=turn(part=3)), dict(t=turn(part=66)),
+               dict(t=turn(part=0)), dict(t=turn(positions=0)), dict(t=turn(table=0)),
+               dict(out=rows(data=(FAKE << 2) + 2)), dict(out=rows(token=256)),
+               dict(out=rows(data=(FAKE << 2) + 256))):
+        refused(call(**kw))
+        assert L.wait_sim_last_error()
+    refused(call(n=1 << 31), B.WS_EUNSUPPORTED)
+    for kw in (dict(n=0), dict(n=0, w=None, t=turn()), dict(n=0, dim=1)):
+        assert call(**kw) == B.WS_OK
+
+
+def test_enter_refusals():
+    L = kv._lib()
+    # queries, keys and values beside one another in rows of 8 vectors of 64
+    q, k, v = (rows(data=(FAKE << 2) + 128 * i, token=512) for i in (0, 4, 6))
+    far = rows(data=FAKE << 3, token=256)
+
+    def call(c=None, q=q, out=far, heads=4, k=k, v=v, slots=FAKE, n=3, qn=norm(), kn=norm(),
+             t=turn()):
+        return L.wait_kv_enter(c or cache(), q, out, heads, k, v, slots, n, qn, kn, t, None)
+
+    for kw in (dict(c=cache(page_size=3)), dict(c=cache(k=0)), dict(c=cache(type=kv.INT8)),
+               dict(n=-1), dict(heads=0), dict(q=rows(data=0)), dict(k=rows(data=0)),
+               dict(v=rows(type=kv.FP16)), dict(q=rows(type=kv.FP32)), dict(slots=None),
+               dict(slots=FAKE + 4), dict(qn=norm(eps=-1.0)), dict(kn=norm(type=9)),
+               dict(t=turn(part=66)), dict(out=rows(data=(FAKE << 2) + 2, token=512)),
+               # in the place of the keys, or across the values
+               dict(out=k), dict(out=rows(data=(FAKE << 2) + 128 * 3, token=512))):
+        refused(call(**kw))
+    refused(call(c=cache(dim=96)), B.WS_EUNSUPPORTED)
+    refused(call(n=1 << 30), B.WS_EUNSUPPORTED)
+    assert call(n=0) == B.WS_OK
+    assert call(n=0, out=q) == B.WS_OK       # the place of the queries itself
+    assert call(n=0, qn=None, kn=None, t=None) == B.WS_OK
+
+
+def batch(**kw):
+    d = dict(table=FAKE, table_stride=8, table_cols=8, starts=FAKE, kv_lens=FAKE, n_seq=2,
+             n_tokens=4, heads=4, scale=1.0, causal=1, window=0, max_q_len=2, max_kv_len=100)
+    d.update(kw)
+    return kv.BATCH.pack(*d.values())
+
+
+def test_weigh_refusals():
+    L = kv._lib()
+
+    def call(c=None, b=None, q=None, lse=FAKE << 3, w=FAKE << 4):
+        return L.wait_kv_weigh(c or cache(), b or batch(), q or rows(), lse, w, 1, None, 0, None)
+
+    for kw in (dict(c=cache(page_size=0)), dict(b=batch(heads=3)), dict(b=batch(heads=0)),
+               dict(b=batch(n_seq=-1)), dict(b=batch(n_tokens=-1)), dict(b=batch(table_cols=-1)),
+               dict(b=batch(scale=0.0)), dict(b=batch(scale=float("nan"))),
+               dict(b=batch(window=-1)), dict(b=batch(max_q_len=-1)),
+               dict(b=batch(max_kv_len=-1)), dict(b=batch(starts=0)), dict(b=batch(kv_lens=0)),
+               dict(b=batch(table=0)), dict(b=batch(table=FAKE + 2)), dict(q=rows(data=0)),
+               dict(q=rows(type=kv.FP32)), dict(q=rows(type=kv.FP16)), dict(lse=None),
+               dict(lse=FAKE + 1), dict(w=None), dict(w=FAKE + 2),
+               dict(w=FAKE << 3), dict(w=FAKE + 64)):       # the log-sums, the keys
+        refused(call(**kw))
+    for kw in (dict(b=batch(n_tokens=1 << 30)), dict(b=batch(table_cols=1 << 26)),
+               dict(c=cache(dim=32))):
+        refused(call(**kw), B.WS_EUNSUPPORTED)
+    assert call(b=batch(n_seq=0)) == B.WS_OK
+    assert call(b=batch(table_cols=0, table=0)) == B.WS_OK
+
+
+def eviction(**kw):
+    d = dict(table=FAKE, table_stride=8, table_cols=8, kv_lens=FAKE, n_seq=2, keep=20, recent=5,
+             to=0, to_stride=2, to_cols=2, max_kv_len=100)
+    d.update(kw)
+    return kv.EVICTION.pack(*d.values())
+
+
+def test_evict_refusals():
+    L = kv._lib()
+
+    def call(c=None, e=None, w=FAKE, kept=FAKE << 2, left=FAKE << 3):
+        return L.wait_kv_evict(c or cache(), e or eviction(), w, kept, left, None)
+
+    for kw in (dict(c=cache(pages=0)), dict(e=eviction(n_seq=-1)), dict(e=eviction(keep=0)),
+               dict(e=eviction(keep=-3)), dict(e=eviction(recent=-1)),
+               dict(e=eviction(recent=21)), dict(e=eviction(table_cols=-1)),
+               dict(e=eviction(table_stride=-1)), dict(e=eviction(max_kv_len=-1)),
+               dict(e=eviction(to=FAKE, to_cols=1)), dict(e=eviction(to=FAKE, to_stride=-1)),
+               dict(e=eviction(to=FAKE + 2)), dict(e=eviction(table=0)),
+               dict(e=eviction(kv_lens=0)), dict(e=eviction(kv_lens=FAKE + 2)), dict(w=None),
+               dict(kept=None), dict(left=None), dict(left=FAKE), dict(left=FAKE + 4)):
+        refused(call(**kw))
+    for kw in (dict(e=eviction(table_cols=1 << 26)), dict(e=eviction(keep=1 << 30)),
+               dict(c=cache(dim=8))):
+        refused(call(**kw), B.WS_EUNSUPPORTED)
+    assert call(e=eviction(n_seq=0)) == B.WS_OK
+
+
+def small(dtype=torch.bfloat16):
+    return kv.Cache.empty(4, 16, 2, 64, dtype, device="cpu")
+
+
+def tensors():
+    return dict(q=torch.zeros(3, 4, 64, dtype=torch.bfloat16),
+                k=torch.zeros(3, 2, 64, dtype=torch.bfloat16),
+                v=torch.zeros(3, 2, 64, dtype=torch.bfloat16), slots=torch.arange(3),
+                w=torch.ones(64), pos=torch.arange(3), table=torch.zeros(10, 64),
+                pages=torch.zeros(1, 2, dtype=torch.int32),
+                starts=torch.tensor([0, 3], dtype=torch.int32),
+                lens=torch.tensor([9], dtype=torch.int32), lse=torch.zeros(3, 4),
+                weights=torch.zeros(4, 2, 16), to=torch.ones(1, 2, dtype=torch.int32))
+
+
+def _norm(t):
+    return kv.norm_rotary(t["q"], t["w"], t["pos"], t["table"])
+
+
+def _enter(t):
+    return kv.enter(small(), t["q"], t["k"], t["v"], t["slots"], positions=t["pos"],
+                    table=t["table"], q_norm=t["w"], k_norm=t["w"])
+
+
+def _weigh(t):
+    return kv.weigh(t["q"], t["lse"], small(), t["pages"], t["starts"], t["lens"], t["weights"])
+
+
+def _evict(t):
+    return kv.evict(small(), t["pages"], t["lens"], t["weights"], keep=4, recent=2, to=t["to"])
+
+
+CALLS = dict(norm=(_norm, ("q", "w", "table")), enter=(_enter, ("q", "k", "v", "w", "table")),
+             weigh=(_weigh, ("q", "lse", "weights")), evict=(_evict, ("weights",)))
+
+
+@pytest.mark.parametrize("call,name", [(c, n) for c, (_, names) in CALLS.items() for n in names])
+def test_gradients_are_refused(call, name):
+    t = tensors()
+    with pytest.raises(ValueError, match="on the GPU"):
+        CALLS[call][0](t)
+    t[name].requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        CALLS[call][0](t)
+    with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
+        CALLS[call][0](t)
+
+
+BAD = [("norm", "w", torch.ones(63)), ("norm", "w", torch.ones(3, 64)),
+       ("norm", "w", torch.ones(64, dtype=torch.int8)), ("norm", "w", torch.ones(4, 128)[:, ::2]),
+       ("norm", "pos", None), ("norm", "table", None), ("norm", "pos", torch.arange(4)),
+       ("norm", "table", torch.zeros(10, 63)), ("norm", "q", torch.zeros(3, 64)),
+       ("enter", "q", torch.zeros(3, 4, 64)), ("enter", "q", torch.zeros(2, 4, 64).bfloat16()),
+       ("enter", "q", torch.zeros(3, 4, 32).bfloat16()),
+       ("enter", "q", torch.zeros(3, 0, 64).bfloat16()),
+       ("enter", "k", torch.zeros(3, 4, 64).bfloat16()), ("enter", "v", torch.zeros(3, 2, 64)),
+       ("enter", "slots", torch.arange(3).int()), ("enter", "slots", torch.arange(4)),
+       ("enter", "pos", None), ("enter", "w", torch.ones(2, 63)),
+       ("weigh", "q", torch.zeros(3, 4, 64)), ("weigh", "q", torch.zeros(3, 4, 64).half()),
+       ("weigh", "q", torch.zeros(3, 3, 64).bfloat16()), ("weigh", "lse", torch.zeros(3, 2)),
+       ("weigh", "lse", torch.zeros(3, 4).half()), ("weigh", "lse", torch.zeros(4, 3).t()),
+       ("weigh", "weights", torch.zeros(4, 16, 2)), ("weigh", "weights", torch.zeros(4, 2, 16).half()),
+       ("weigh", "starts", torch.zeros(1, dtype=torch.int32)), ("weigh", "lens", torch.tensor([9])),
+       ("weigh", "pages", torch.zeros(1, 2)), ("evict", "pages", torch.zeros(1, 2)),
+       ("evict", "pages", torch.zeros(2, dtype=torch.int32)),
+       ("evict", "lens", torch.zeros(2, dtype=torch.int32)),
+       ("evict", "weights", torch.zeros(3, 2, 16)), ("evict", "to", torch.ones(1, 2)),
+       ("evict", "to", torch.ones(1, 0, dtype=torch.int32)),
+       ("evict", "to", torch.ones(2, 2, dtype=torch.int32))]
+
+
+@pytest.mark.parametrize("which", range(len(BAD)))
+def test_python_refusals(which):
+    call, name, value = BAD[which]
+    t = tensors()
+    t[name] = value
+    with pytest.raises(ValueError) as e:
+        CALLS[call][0](t)
+    assert "on the GPU" not in str(e.value)
+
+
+def test_more_python_refusals():
+    t = tensors()
+    for eps in (-1.0, float("nan"), float("inf")):
+        with pytest.raises((ValueError, B.WaitSimError)):
+            kv.norm_rotary(t["q"], t["w"], eps=eps)
+    for kw in (dict(keep=0), dict(keep=4, recent=5), dict(keep=4, recent=-1), dict(keep=1 << 31)):
+        with pytest.raises(ValueError, match="keep|kept"):
+            kv.evict(small(), t["pages"], t["lens"], t["weights"], **kw)
+    with pytest.raises(ValueError, match="shape"):
+        kv.enter(small(), t["q"], t["k"], t["v"], t["slots"], out=t["k"])
+    with pytest.raises(ValueError, match="overlap"):
+        kv.norm_rotary(t["q"], out=torch.zeros(1, 4, 64, dtype=torch.bfloat16).expand(3, 4, 64))
+    for call in (lambda: kv.norm_rotary([1.0]), lambda: kv.norm_rotary(t["q"], [1.0]),
+                 lambda: kv.norm_rotary(t["q"], eps="x"), lambda: kv.evict(small(), 3, t["lens"], t["weights"], keep=3),
+                 lambda: kv.weigh(t["q"], None, small(), t["pages"], t["starts"], t["lens"], t["weights"]),
+                 lambda: kv.evict(small(), t["pages"], t["lens"], t["weights"], keep="4")):
+        with pytest.raises(TypeError):
+            call()
+
+
+def test_weigh_workspace_is_the_librarys():
+    t = tensors()
+    for kw in (dict(), dict(max_q_len=1), dict(max_kv_len=5), dict(causal=False, window=3)):
+        n = kv.weigh_workspace_bytes(t["q"], small(), t["pages"], t["starts"], t["lens"], **kw)
+        assert n >= 0 and n % 4 == 0
+    with pytest.raises(B.WaitSimError):
+        kv.weigh_workspace_bytes(t["q"], small(), t["pages"], t["starts"], t["lens"], window=-1)
+
+
+def test_the_oracles_choice():
+    """Ties, NaN, zeros of both signs, in the definition that kernels are held to."""
+    nan, inf = float("nan"), float("inf")
+    w = torch.tensor([1.0, 1.0, 0.0, -0.0, nan, inf, 2.0, 1.0])
+    assert kept_keys(w, 3, 0) == [4, 5, 6]
+    assert kept_keys(w, 4, 0) == [0, 4, 5, 6]
+    assert kept_keys(w, 4, 2) == [4, 5, 6, 7]
+    assert kept_keys(w, 7, 0) == [0, 1, 2, 4, 5, 6, 7]
+    assert kept_keys(w, 7, 7) == list(range(1, 8))
+    assert kept_keys(w, 8, 3) == list(range(8)) and kept_keys(w[:0], 8, 3) == []
