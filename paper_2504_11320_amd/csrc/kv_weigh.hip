@@ -28,6 +28,7 @@ struct Args {
   const int32_t *starts, *lens;
   int32_t n_seq, n_tokens;
   int32_t heads, kv_heads, group;
+  uint32_t by_group;  // 2^32 / group, rounded up: a whole quotient of small numbers
   int32_t pages, page_shift;
   float scale;  // times log2(e)
   int32_t causal, window, accumulate;
@@ -211,17 +212,18 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {
 #pragma unroll
       for (int t = 0; t < F::tiles; ++t) {
         const float f = CODES ? __shfl(factor, 16 * t + n16) : factor;
-        Range see = {0, 16};
-        if (!all) {
-          see = rows_of_key(a, s, k0 + 16 * t + n16, rows);
-          see.lo -= r0 + 4 * g;
-          see.hi -= r0 + 4 * g;
-        }
+        float p[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = exp2_of(__builtin_fmaf(z[t][r], f, -log[r]));
-          sum[t] += all || (r >= see.lo && r < see.hi) ? p : 0.0f;
+        for (int r = 0; r < 4; ++r) p[r] = exp2_of(__builtin_fmaf(z[t][r], f, -log[r]));
+        if (!all) {
+          const Range see = rows_of_key(a, s, k0 + 16 * t + n16, rows);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int32_t row = r0 + 4 * g + r;
+            p[r] = ((row >= see.lo) & (row < see.hi)) ? p[r] : 0.0f;
+          }
         }
+        sum[t] += (p[0] + p[1]) + (p[2] + p[3]);
       }
     }
     float own = 0.0f;
@@ -238,12 +240,12 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {
 
 // ------------------------------------------------------- many rows ------
 //
-// A wave keeps 64 keys (32 of D = 256) in registers as the products' left
-// operands; the rows come through shared memory, three blocks of 64 in turn, one
-// in use and two on their way.  With the keys as rows of the product a lane has
-// one row's log-sum and 16 keys' sums of each 32, which it adds up in registers
-// until the end.  Where there are few keys for many rows, the rows are split over
-// workgroups too and a second kernel adds the parts in their order.
+// A wave keeps 64 keys (32 of D = 256) in registers as the products' right
+// operands; the rows come through shared memory, three blocks of 64 (32) in turn,
+// one in use and two on their way.  The products of 32 rows run beside the
+// exponentials of the 32 before.  Where there are few keys for many rows, the
+// rows are split over workgroups too and a second kernel adds the parts in their
+// order.
 
 template <int TYPE, int D>
 struct Many {
@@ -256,15 +258,23 @@ struct Many {
   static constexpr int chunks = D / 8;             // of 16 bytes, of a row
   static constexpr int copies = rows * chunks / 256;  // of a thread, of a block
   static constexpr int side = rows * row_bytes;
-  static constexpr int block = side + rows * 4;    // and the log-sums
-  static constexpr int smem = 3 * block;
+  static constexpr int smem = 3 * side + 4 * rows * 4;  // and the log-sums of four blocks
 };
 
-// 4 bytes a lane from memory to shared memory, as copy_to_lds.
-__device__ __forceinline__ void copy_word_to_lds(const float *from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+constexpr int kAhead = 3;  // products whose operands are under way
+
+// 16 bytes, or 4, a lane from memory to shared memory: as copy_to_lds, from an
+// address for all lanes and an offset of each.
+__device__ __forceinline__ void copy_from(const void *base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :
-               : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to))
+               : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
+               : "memory");
+}
+__device__ __forceinline__ void copy_word_from(const void *base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
                : "memory");
 }
 // Copies but the last N of this wave have arrived.
@@ -272,7 +282,7 @@ template <int N>
 __device__ __forceinline__ void await_copies_but() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-// All waves are here, and have read what they asked of shared memory.
+// All waves are here, and have read and written what they asked of shared memory.
 __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -308,9 +318,10 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
   using M = Many<TYPE, D>;
   constexpr bool CODES = kCodes<TYPE>;
   constexpr int own = 32 * M::ktiles;  // keys of a wave
+  constexpr int tiles = M::rows / 32;  // of a block's rows
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n32 = lane & 31, hh = lane >> 5;
+  const int n32 = lane & 31, hh = lane >> 5, mine = lane & (own - 1);
   // the first keys have most rows, and go first
   const int32_t pairs = a.n_seq * a.kv_heads;
   const int32_t pair = id % pairs, part = id / pairs % a.parts;
@@ -320,38 +331,103 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
   if (rows <= kFewRows) return;
   const int32_t end = min(s.m, a.capacity);
   const uint32_t shared = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  float *const logs = (float *)(smem + 3 * M::side);
 
   for (int32_t tile = id / pairs / a.parts; tile * M::keys < end; tile += a.tiles) {
     const Parts split = parts_of<TYPE, D>(a, s, tile, end);
     if (part >= split.parts) continue;
     const int32_t lo = split.lo + part * split.each, hi = min(split.hi, lo + split.each);
-    const int32_t k0 = tile * M::keys + wave * own;  // this wave's keys
+    const int32_t blocks = hi > lo ? (hi - lo + M::rows - 1) / M::rows : 0;
+    const int32_t k0 = tile * M::keys + wave * own, key = k0 + mine;  // the wave's and the lane's
+    const int32_t row_at = cache_row(a, page_entry(a, b, key, end), h, key, end);
+
     // the keys, in the layout of the product
     u32x4 k[M::ktiles][M::steps];
-    float f[CODES ? M::ktiles : 1][16];
+    float f[M::ktiles];
 #pragma unroll
     for (int t = 0; t < M::ktiles; ++t) {
-      const int32_t key = k0 + 32 * t + n32;
-      const int64_t r = max(cache_row(a, page_entry(a, b, key, end), h, key, end), 0);
+      const int64_t r = max(__shfl(row_at, 32 * t + n32), 0);
       const char *p = a.k + r * (D * M::esz) + 16 * hh;
-      if constexpr (CODES) {
-        const float scale = a.scale * a.ks[r];
+      f[t] = CODES ? a.ks[r] : 1.0f;
 #pragma unroll
-        for (int i = 0; i < M::steps / 2; ++i)
-          codes_to_16<TYPE, BF>(*reinterpret_cast<const u32x4 *>(p + 32 * i), k[t][2 * i],
-                                k[t][2 * i + 1]);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) f[t][r] = __shfl(scale, 8 * (r / 4) + 4 * hh + r % 4);
-      } else {
-#pragma unroll
-        for (int i = 0; i < M::steps; ++i) k[t][i] = *reinterpret_cast<const u32x4 *>(p + 32 * i);
-      }
+      for (int i = 0; i < M::steps / (CODES ? 2 : 1); ++i)
+        k[t][CODES ? 2 * i : i] = *reinterpret_cast<const u32x4 *>(p + 32 * i);
     }
-    // the key whose sum this lane has in the end
-    const int32_t key = k0 + (M::ktiles == 2 ? 32 * (n32 & 1) : 0) + 8 * (n32 >> 3) + 4 * hh +
-                        ((n32 >> 1) & 3);
-    const int32_t row_at = cache_row(a, page_entry(a, b, key, end), h, key, end);
-    const float was = old_weight(a, s, key, row_at);
+    float had = old_weight(a, s, key, row_at);
+
+    // A block's copies: its first row is head g0 of token t0, and its row r lies
+    // r + g0 heads behind that token's first.  Blocks go from the last rows to the
+    // first: the workgroups of a head that run together then read the same ones.
+    const int32_t first = lo + (blocks - 1) * M::rows, t0 = first / a.group;
+    const int32_t turn = M::rows / a.group, rest = M::rows - turn * a.group;
+    const char *qbase = (const char *)(a.q + (int64_t)(s.q0 + t0) * a.qt + (int64_t)h * a.group * a.qh);
+    const float *lbase = a.lse + (int64_t)(s.q0 + t0) * a.heads + h * a.group;
+    int32_t g0 = first - t0 * a.group, l0 = g0;
+    const int32_t row_of_copy = (int)threadIdx.x / M::chunks;  // and 256 / chunks further each
+    const int32_t row_of_log = wave * (M::rows / 4) + (lane & (M::rows / 4 - 1));
+    auto token_of = [&](int32_t x) {
+      return a.group == 1 ? x : (int32_t)__umulhi((uint32_t)x, a.by_group);
+    };
+    auto q_offset = [&](int32_t r, int32_t x) {
+      const int32_t t = token_of(x);
+      return (uint32_t)t * (uint32_t)(2 * a.qt) + (uint32_t)(x - t * a.group) * (uint32_t)(2 * a.qh) +
+             16u * ((threadIdx.x % M::chunks) ^ row_swizzle<D>(r));
+    };
+    auto log_offset = [&](int32_t x) {
+      const int32_t t = token_of(x);
+      return (uint32_t)(t * a.heads + x - t * a.group) * 4u;
+    };
+    // Offsets change where heads do not fill blocks, and behind the last block, the
+    // first one here, whose rows behind the last are that row again.
+    uint32_t off[M::copies], log_off = 0;
+    // the queries of the block at row r0
+    auto copy_rows = [&](int32_t r0, int buffer) {
+      const uint32_t to = shared + buffer * M::side;
+      const bool anew = rest || r0 + M::rows >= first;
+#pragma unroll
+      for (int i = 0; i < M::copies; ++i) {
+        const int32_t r = row_of_copy + i * (256 / M::chunks);
+        if (anew) off[i] = q_offset(r, g0 + min(r, rows - 1 - r0));
+        copy_from(qbase, off[i], to + (i * 256 + wave * 64) * 16);
+      }
+      qbase -= (int64_t)turn * a.qt * 2;
+      g0 -= rest;
+      if (g0 < 0) {
+        g0 += a.group;
+        qbase -= a.qt * 2;
+      }
+    };
+    // and their log-sums, a quarter for each wave; of a block that is not there
+    // something else, since copies are counted
+    auto copy_logs = [&](int32_t r0, int slot) {
+      if (rest || r0 + M::rows >= first) log_off = log_offset(l0 + min(row_of_log, rows - 1 - r0));
+      if (lane < M::rows / 4)
+        copy_word_from(r0 >= lo ? lbase : a.lse, r0 >= lo ? log_off : 0,
+                       shared + 3 * M::side + (slot * M::rows + wave * (M::rows / 4)) * 4);
+      lbase -= (int64_t)turn * a.heads;
+      l0 -= rest;
+      if (l0 < 0) {
+        l0 += a.group;
+        lbase -= a.heads;
+      }
+    };
+    // as they are subtracted, by the wave that copied them
+    auto ready_logs = [&](int slot) {
+      if (lane < M::rows / 4) {
+        float *p = logs + slot * M::rows + row_of_log;
+        *p = -row_log(*p);
+      }
+    };
+    meet();  // nobody reads what an earlier turn left
+    if (blocks > 0) {
+      copy_logs(first, 0);
+      copy_rows(first, 0);
+      copy_logs(first - M::rows, 1);
+    }
+    if (blocks > 1) {
+      copy_rows(first - M::rows, 1);
+      copy_logs(first - 2 * M::rows, 2);
+    }
     // rows that see some of the wave's keys, and those that see all of them
     const int32_t last = min(k0 + own, end) - 1;
     Range some = {0, 0}, every = {0, 0};
@@ -360,147 +436,148 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
       some = {at_first.lo, min(at_last.hi, hi)};
       every = {at_last.lo, min(at_first.hi, hi)};
     }
-
-    // copies: rows of this thread's, and where they are
-    const char *from[M::copies];
-    int32_t head[M::copies];
-    auto row_at_q = [&](int32_t row, int32_t *in) {
-      const int32_t token = row / a.group;
-      *in = row - token * a.group;
-      return (const char *)(a.q + (int64_t)(s.q0 + token) * a.qt + (int64_t)(h * a.group + *in) * a.qh);
-    };
-    auto row_of_copy = [&](int i) { return (i * 256 + (int)threadIdx.x) / M::chunks; };
 #pragma unroll
-    for (int i = 0; i < M::copies; ++i) {
-      const int r = row_of_copy(i);
-      from[i] = row_at_q(min(lo + r, rows - 1), &head[i]) +
-                16 * ((int)threadIdx.x % M::chunks ^ row_swizzle<D>(r));
+    for (int t = 0; t < M::ktiles; ++t) {
+      f[t] *= a.scale;
+      if constexpr (CODES) {
+#pragma unroll
+        for (int i = 0; i < M::steps; i += 2) codes_to_16<TYPE, BF>(k[t][i], k[t][i], k[t][i + 1]);
+      }
+      // waited for here: a wait in the loop would be for the copies too
+#pragma unroll
+      for (int i = 0; i < M::steps; ++i) asm volatile("" : "+v"(k[t][i]));
+      asm volatile("" : "+v"(f[t]));
     }
-    int32_t unused;
-    const char *end_row = row_at_q(rows - 1, &unused);
-    // log-sums: a quarter of a block for each wave
-    constexpr int quarter = M::rows / 4;
-    const int32_t log_row = wave * quarter + (lane & (quarter - 1));
-    int32_t log_in = (lo + log_row) % a.group;
-    int64_t log_at = (int64_t)(s.q0 + (lo + log_row) / a.group) * a.heads + h * a.group + log_in;
-    const int64_t log_end = (int64_t)(s.q0 + s.n) * a.heads + h * a.group + a.group - 1 - a.heads;
-    const int32_t turn = M::rows / a.group, rest = M::rows - turn * a.group;
-    const int64_t ahead = ((int64_t)turn * a.qt + (int64_t)rest * a.qh) * 2;
-    const int64_t carry = (a.qt - (int64_t)a.group * a.qh) * 2;
-    auto copy = [&](int32_t r0, int buffer) {
-      const uint32_t to = shared + buffer * M::block;
-      const bool cut = r0 + M::rows > rows;
+    asm volatile("" : "+v"(had));
+
+    float sum[M::ktiles][2] = {};
+    f32x16 za[M::ktiles], zb[M::ktiles];
+    f32x4 logs_of[4];         // of the rows that wait for their exponentials
+    int32_t waiting = 0;      // 0: none do, 1: all keys see them, 2: not all
+    int32_t waiting_row = 0;  // the first of them
+    // Element r of 16 is row 8 (r / 4) + 4 hh + r % 4.
+    auto add = [&](const f32x16 (&z)[M::ktiles], int e) {
+      const int t = e / 16, r = e % 16;
+      sum[t][r & 1] += exp2_of(__builtin_fmaf(z[t][r], f[t], logs_of[r / 4][r % 4]));
+    };
+    auto add_seen = [&](const f32x16 (&z)[M::ktiles]) {
 #pragma unroll
-      for (int i = 0; i < M::copies; ++i) {
-        const int r = row_of_copy(i);
-        const char *p = from[i];
-        if (cut && r0 + r >= rows)
-          p = end_row + 16 * ((int)threadIdx.x % M::chunks ^ row_swizzle<D>(r));
-        copy_to_lds(p, to + (i * 256 + wave * 64) * 16);
-        from[i] += ahead;
-        if (rest) {
-          head[i] += rest;
-          if (head[i] >= a.group) {
-            head[i] -= a.group;
-            from[i] += carry;
-          }
+      for (int t = 0; t < M::ktiles; ++t) {
+        Range see = rows_of_key(a, s, k0 + 32 * t + n32, rows);
+        see.lo -= waiting_row + 4 * hh;
+        see.hi = min(see.hi, hi) - (waiting_row + 4 * hh);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = exp2_of(__builtin_fmaf(z[t][r], f[t], logs_of[r / 4][r % 4]));
+          const int at = 8 * (r / 4) + r % 4;
+          sum[t][r & 1] += ((at >= see.lo) & (at < see.hi)) ? p : 0.0f;
         }
       }
-      if (lane < quarter)
-        copy_word_to_lds(a.lse + min(log_at, log_end), to + M::side + wave * quarter * 4);
-      log_at += (int64_t)turn * a.heads + rest;
-      log_in += rest;
-      if (log_in >= a.group) {
-        log_in -= a.group;
-        log_at += a.heads - a.group;
+    };
+    auto read = [&](const char *q, int e) {
+      const int c = CODES ? 4 * (e / 2) + 2 * hh + e % 2 : 2 * e + hh;
+      return *reinterpret_cast<const u32x4 *>(q + (c ^ row_swizzle<D>(n32)) * 16);
+    };
+    auto product = [&](f32x16 (&z)[M::ktiles], u32x4 x, int e) {
+#pragma unroll
+      for (int t = 0; t < M::ktiles; ++t) z[t] = mfma32<BF>(x, k[t][e], z[t]);
+    };
+    // One block of 32 rows into z, beside what waits in `before`.
+    auto step = [&](f32x16 (&z)[M::ktiles], const f32x16 (&before)[M::ktiles], const char *q,
+                    const float *log, int32_t w0) {
+      const bool none = w0 >= some.hi || w0 + 32 <= some.lo;
+      if (waiting == 1 && !none) {
+#pragma unroll
+        for (int t = 0; t < M::ktiles; ++t) z[t] = f32x16{};
+        // operands are asked for kAhead products before theirs, and each product's
+        // share of the exponentials stays behind it
+        u32x4 x[M::steps];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) x[e] = read(q, e);
+        constexpr int per = 16 * M::ktiles / M::steps;
+#pragma unroll
+        for (int e = 0; e < M::steps; ++e) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (e + kAhead < M::steps) x[e + kAhead] = read(q, e + kAhead);
+          product(z, x[e], e);
+#pragma unroll
+          for (int i = 0; i < per; ++i) add(before, e * per + i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        if (waiting == 1) {
+#pragma unroll
+          for (int e = 0; e < 16 * M::ktiles; ++e) add(before, e);
+        } else if (waiting == 2) {
+          add_seen(before);
+        }
+        if (!none) {
+#pragma unroll
+          for (int t = 0; t < M::ktiles; ++t) z[t] = f32x16{};
+#pragma unroll
+          for (int e = 0; e < M::steps; ++e) product(z, read(q, e), e);
+        }
+      }
+      waiting = none ? 0 : w0 >= every.lo && w0 + 32 <= every.hi ? 1 : 2;
+      waiting_row = w0;
+      if (!none) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) logs_of[i] = *reinterpret_cast<const f32x4 *>(log + 8 * i + 4 * hh);
       }
     };
 
-    float sum[M::ktiles][16];
-#pragma unroll
-    for (int t = 0; t < M::ktiles; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sum[t][r] = 0.0f;
-
-    const int32_t blocks = hi > lo ? (hi - lo + M::rows - 1) / M::rows : 0;
-    meet();  // nobody reads what an earlier turn left
-    for (int i = 0; i < 2 && i < blocks; ++i) copy(lo + i * M::rows, i);
     int buffer = 0;
     for (int32_t i = 0; i < blocks; ++i) {
+      // the queries of this block and the log-sums of the next are there
       if (i + 1 < blocks)
         await_copies_but<M::copies + 1>();
       else
         await_copies();
+      if (i == 0) ready_logs(0);
       meet();
-      const int32_t r0 = lo + i * M::rows;
-      if (i + 2 < blocks) copy(r0 + 2 * M::rows, buffer == 0 ? 2 : buffer - 1);
-      const char *q = smem + buffer * M::block;
-      const float *logs = (const float *)(q + M::side);
-#pragma unroll
-      for (int u = 0; u < M::rows / 32; ++u) {
-        const int32_t w0 = r0 + 32 * u;
-        if (w0 >= some.hi || w0 + 32 <= some.lo) continue;
-        const float log = row_log(logs[32 * u + n32]);
-        f32x16 z[M::ktiles];
-#pragma unroll
-        for (int t = 0; t < M::ktiles; ++t) z[t] = f32x16{};
-#pragma unroll
-        for (int e = 0; e < M::steps; ++e) {
-          const int c = CODES ? 4 * (e / 2) + 2 * hh + e % 2 : 2 * e + hh;
-          const u32x4 x = *reinterpret_cast<const u32x4 *>(
-              q + (32 * u + n32) * M::row_bytes + (c ^ row_swizzle<D>(n32)) * 16);
-#pragma unroll
-          for (int t = 0; t < M::ktiles; ++t) z[t] = mfma32<BF>(k[t][e], x, z[t]);
-        }
-        if (w0 >= every.lo && w0 + 32 <= every.hi) {
-#pragma unroll
-          for (int t = 0; t < M::ktiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              sum[t][r] += exp2_of(__builtin_fmaf(z[t][r], CODES ? f[t][r] : a.scale, -log));
-        } else {
-          const int32_t row = w0 + n32;
-          Range see = {0, 0};
-          if (row < hi) see = token_range(a, s, row / a.group);
-#pragma unroll
-          for (int t = 0; t < M::ktiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int32_t j = k0 + 32 * t + 8 * (r / 4) + 4 * hh + r % 4;
-              const float p = exp2_of(__builtin_fmaf(z[t][r], CODES ? f[t][r] : a.scale, -log));
-              sum[t][r] += j >= see.lo && j < see.hi ? p : 0.0f;
-            }
-        }
+      const int32_t r0 = first - i * M::rows;
+      if (i + 2 < blocks) {
+        copy_rows(r0 - 2 * M::rows, buffer == 0 ? 2 : buffer - 1);
+        copy_logs(r0 - 3 * M::rows, (i + 3) & 3);
+      }
+      if (i + 1 < blocks) ready_logs((i + 1) & 3);
+      const char *q = smem + buffer * M::side + n32 * M::row_bytes;
+      const float *log = logs + (i & 3) * M::rows;
+      if constexpr (tiles == 2) {
+        step(za, zb, q, log, r0);
+        step(zb, za, q + 32 * M::row_bytes, log + 32, r0 + 32);
+      } else if (i & 1) {
+        step(zb, za, q, log, r0);
+      } else {
+        step(za, zb, q, log, r0);
       }
       buffer = buffer == 2 ? 0 : buffer + 1;
     }
-    // over the 32 rows' lanes: each step halves the keys that a lane has
-    auto fold = [&](float a0, float a1, int m) {
-      const bool up = lane & m;
-      return (up ? a1 : a0) + __shfl_xor(up ? a0 : a1, m);
+    auto finish = [&](const f32x16 (&z)[M::ktiles]) {
+      if (waiting == 1) {
+#pragma unroll
+        for (int e = 0; e < 16 * M::ktiles; ++e) add(z, e);
+      } else if (waiting == 2) {
+        add_seen(z);
+      }
     };
-    float one[M::ktiles];
-#pragma unroll
-    for (int t = 0; t < M::ktiles; ++t) {
-#pragma unroll
-      for (int r = 0; r < 8; ++r) sum[t][r] = fold(sum[t][r], sum[t][r + 8], 16);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sum[t][r] = fold(sum[t][r], sum[t][r + 4], 8);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) sum[t][r] = fold(sum[t][r], sum[t][r + 2], 4);
-      one[t] = fold(sum[t][0], sum[t][1], 2);
-    }
-    float total;
-    if constexpr (M::ktiles == 2)
-      total = fold(one[0], one[1], 1);
+    if (tiles == 2 || blocks % 2 == 0)
+      finish(zb);
     else
-      total = one[0] + __shfl_xor(one[0], 1);
-    const bool mine = key < end && (M::ktiles == 2 || (lane & 1) == 0);
+      finish(za);
+    // the two halves' rows
+    float total = sum[0][0] + sum[0][1];
+    if constexpr (M::ktiles == 2) {
+      const float other = sum[1][0] + sum[1][1];
+      total = (hh ? other : total) + __shfl_xor(hh ? total : other, 32);
+    } else {
+      total += __shfl_xor(total, 32);
+    }
+    const bool has = key < end && lane < own;
     if (split.parts > 1) {
-      if (mine)
-        a.sums[((int64_t)part * pairs + pair) * a.tiles * M::keys + key] = total;
-    } else if (mine && row_at != kNoRow) {
-      a.weights[row_at] = was + total;
+      if (has) a.sums[((int64_t)part * pairs + pair) * a.tiles * M::keys + key] = total;
+    } else if (has && row_at != kNoRow) {
+      a.weights[row_at] = had + total;
     }
   }
 }
@@ -667,8 +744,14 @@ int wait_kv_weigh(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_k
     if (L.bytes && (!d_workspace || ws_bytes < (size_t)L.bytes))
       return ws_record_failure(WS_EWORKSPACE, "weigh: the workspace is too small");
     if ((uintptr_t)d_workspace % 4) return invalid("weigh: the workspace must be aligned to 4 bytes");
-    // many rows are copied 16 bytes at a time
-    if (!aligned(*q, 16)) L.many = false;
+    // many rows are copied 16 bytes at a time, a block's from one address with
+    // offsets of 32 bits
+    const int64_t group = b.heads / cache->kv_heads, block = 64 / group + 2;
+    if (!aligned(*q, 16) || group > 4096 || q->token_stride < 0 || q->head_stride < 0 ||
+        q->token_stride >= (int64_t)1 << 31 || q->head_stride >= (int64_t)1 << 31 ||
+        2 * (block * q->token_stride + group * q->head_stride) >= (int64_t)1 << 32 ||
+        4 * block * b.heads >= (int64_t)1 << 32)
+      L.many = false;
     Args a{};
     a.q = (const uint16_t *)q->data;
     a.qt = q->token_stride;
@@ -687,6 +770,7 @@ int wait_kv_weigh(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_k
     a.heads = b.heads;
     a.kv_heads = cache->kv_heads;
     a.group = b.heads / cache->kv_heads;
+    a.by_group = (uint32_t)((((int64_t)1 << 32) + a.group - 1) / a.group);
     a.pages = cache->pages;
     a.page_shift = log2_of(cache->page_size);
     a.scale = (float)((double)b.scale * 1.4426950408889634074);
