@@ -63,13 +63,21 @@ typedef struct {
   const int32_t *to; /* NULL: in place */
   int64_t to_stride;
   int32_t to_cols;    /* at least keep / page_size, rounded up */
-  int32_t max_kv_len; /* upper bound that the launch is laid out for */
+  /* Upper bound that the launch is laid out for.  Requests that are longer are
+   * right all the same, only slower. */
+  int32_t max_kv_len;
 } ws_kv_eviction;
 
+/* Bytes of workspace that wait_kv_evict takes (0 where requests are short). */
+int wait_kv_evict_workspace_bytes(const ws_kv_cache *cache, const ws_kv_eviction *eviction,
+                                  size_t *bytes);
+
 /* kept [n_seq][kv_heads][keep] int32: the kept keys' indices, -1 behind them;
- * new_lens [n_seq]: min(kv_lens, keep), in memory of its own. */
+ * new_lens [n_seq]: min(kv_lens, keep), in memory of its own.  The workspace holds
+ * nothing between calls; calls that overlap need one each. */
 int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, float *weights,
-                  int32_t *kept, int32_t *new_lens, void *hip_stream);
+                  int32_t *kept, int32_t *new_lens, void *d_workspace, size_t ws_bytes,
+                  void *hip_stream);
 
 #ifdef __cplusplus
 }

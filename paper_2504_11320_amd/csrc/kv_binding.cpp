@@ -36,6 +36,7 @@ decltype(&wait_kv_norm_rotary) f_norm_rotary;
 decltype(&wait_kv_enter) f_enter;
 decltype(&wait_kv_weigh_workspace_bytes) f_weigh_workspace;
 decltype(&wait_kv_weigh) f_weigh;
+decltype(&wait_kv_evict_workspace_bytes) f_evict_workspace;
 decltype(&wait_kv_evict) f_evict;
 PyObject *g_check, *g_stream, *g_device, *g_on;  // of binding.py and torch
 
@@ -681,57 +682,93 @@ PyObject *weigh(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
   });
 }
 
+// The eviction and its workspace's bytes.
+ws_kv_eviction eviction_of(const ws_kv_cache &c, int index, PyObject *pages_, PyObject *lens_,
+                           PyObject *keep_, PyObject *recent_, PyObject *to_, PyObject *max_kv,
+                           size_t *bytes) {
+  const at::Tensor &pages = tensor(pages_, "pages"), &lens = tensor(lens_, "kv_lens");
+  const at::Tensor *to = tensor_or_none(to_, "to");
+  for (const at::Tensor *t : {&pages, to})
+    if (t && !(t->dim() == 2 && t->scalar_type() == at::kInt && t->size(0) == pages.size(0) &&
+               (t->size(1) <= 1 || t->stride(1) == 1) && index_of(*t) == index))
+      refuse("%s must be [requests, pages], int32, rows contiguous, on the cache's device",
+             t == to ? "to" : "pages");
+  const int64_t n_seq = pages.size(0), keep = whole(keep_), recent = whole(recent_);
+  need(lens.dim() == 1 && lens.size(0) == n_seq && lens.scalar_type() == at::kInt &&
+           lens.is_contiguous() && index_of(lens) == index,
+       "kv_lens must be one int32 a request, contiguous, on the cache's device");
+  need(n_seq <= INT32_MAX && pages.size(1) <= INT32_MAX && (!to || to->size(1) <= INT32_MAX),
+       "the batch is too large");
+  need(keep >= 1 && keep <= INT32_MAX, "at least one key must be kept, and fewer than 2^31");
+  need(recent >= 0 && recent <= keep, "recent must be 0 to keep");
+  const int64_t capacity = std::min<int64_t>(pages.size(1) * c.page_size, INT32_MAX);
+  ws_kv_eviction e{};
+  e.table = pages.data_ptr<int32_t>();
+  e.table_stride = n_seq > 1 ? pages.stride(0) : pages.size(1);
+  e.table_cols = (int32_t)pages.size(1);
+  e.kv_lens = lens.data_ptr<int32_t>();
+  e.n_seq = (int32_t)n_seq;
+  e.keep = (int32_t)keep;
+  e.recent = (int32_t)recent;
+  if (to) {
+    need(to->size(1) * c.page_size >= keep, "to must have pages for the kept rows");
+    e.to = to->data_ptr<int32_t>();
+    e.to_stride = n_seq > 1 ? to->stride(0) : to->size(1);
+    e.to_cols = (int32_t)to->size(1);
+  }
+  const int64_t bound = max_kv == Py_None ? capacity : std::min<int64_t>(whole(max_kv), capacity);
+  e.max_kv_len = (int32_t)std::max<int64_t>(bound, -1);
+  check(f_evict_workspace(&c, &e, bytes));
+  return e;
+}
+
+// evict_workspace_bytes(cache bytes, GPU, pages, kv_lens, keep, recent, to or None, max_kv or None)
+PyObject *evict_workspace_bytes(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+  ARGS(8)
+  return guarded([&]() -> PyObject * {
+    const ws_kv_cache c = cache_of(v[0]);
+    size_t bytes = 0;
+    eviction_of(c, (int)whole(v[1]), v[2], v[3], v[4], v[5], v[6], v[7], &bytes);
+    return PyLong_FromSize_t(bytes);
+  });
+}
+
 // evict(cache bytes, GPU, the cache's tensors, pages, kv_lens, weights, keep, recent, to or None,
-//       max_kv or None): (kept, new lengths)
+//       max_kv or None, workspace or None): (kept, new lengths)
 PyObject *evict(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
-  ARGS(10)
+  ARGS(11)
   return guarded([&]() -> PyObject * {
     const ws_kv_cache c = cache_of(v[0]);
     const int index = (int)whole(v[1]);
     need(PyTuple_Check(v[2]), "not a cache");
-    const at::Tensor &pages = tensor(v[3], "pages"), &lens = tensor(v[4], "kv_lens");
-    const at::Tensor *to = tensor_or_none(v[8], "to");
-    for (const at::Tensor *t : {&pages, to})
-      if (t && !(t->dim() == 2 && t->scalar_type() == at::kInt && t->size(0) == pages.size(0) &&
-                 (t->size(1) <= 1 || t->stride(1) == 1) && index_of(*t) == index))
-        refuse("%s must be [requests, pages], int32, rows contiguous, on the cache's device",
-               t == to ? "to" : "pages");
-    const int64_t n_seq = pages.size(0), keep = whole(v[6]), recent = whole(v[7]);
-    need(lens.dim() == 1 && lens.size(0) == n_seq && lens.scalar_type() == at::kInt &&
-             lens.is_contiguous() && index_of(lens) == index,
-         "kv_lens must be one int32 a request, contiguous, on the cache's device");
-    need(n_seq <= INT32_MAX && pages.size(1) <= INT32_MAX && (!to || to->size(1) <= INT32_MAX),
-         "the batch is too large");
-    need(keep >= 1 && keep <= INT32_MAX, "at least one key must be kept, and fewer than 2^31");
-    need(recent >= 0 && recent <= keep, "recent must be 0 to keep");
+    size_t bytes = 0;
+    const ws_kv_eviction e = eviction_of(c, index, v[3], v[4], v[6], v[7], v[8], v[9], &bytes);
     const at::Tensor &weights = weights_of(v[5], c, index);
-    const int64_t capacity = std::min<int64_t>(pages.size(1) * c.page_size, INT32_MAX);
-    ws_kv_eviction e{};
-    e.table = pages.data_ptr<int32_t>();
-    e.table_stride = n_seq > 1 ? pages.stride(0) : pages.size(1);
-    e.table_cols = (int32_t)pages.size(1);
-    e.kv_lens = lens.data_ptr<int32_t>();
-    e.n_seq = (int32_t)n_seq;
-    e.keep = (int32_t)keep;
-    e.recent = (int32_t)recent;
-    if (to) {
-      need(to->size(1) * c.page_size >= keep, "to must have pages for the kept rows");
-      e.to = to->data_ptr<int32_t>();
-      e.to_stride = n_seq > 1 ? to->stride(0) : to->size(1);
-      e.to_cols = (int32_t)to->size(1);
-    }
-    const int64_t bound = v[9] == Py_None ? capacity : std::min<int64_t>(whole(v[9]), capacity);
-    e.max_kv_len = (int32_t)std::max<int64_t>(bound, -1);
     need(index >= 0, "the operators run on the GPU");
-    at::Tensor kept = at::empty({n_seq, c.kv_heads, keep}, pages.options()),
-               left = at::empty({n_seq}, lens.options());
+    const auto options = weights.options().dtype(at::kInt);
+    at::Tensor kept = at::empty({e.n_seq, c.kv_heads, e.keep}, options),
+               left = at::empty({e.n_seq}, options), space;
+    void *ptr = nullptr;
+    size_t have = 0;
+    if (v[10] != Py_None) {
+      const at::Tensor &t = tensor(v[10], "workspace");
+      need(t.is_contiguous() && index_of(t) == index,
+           "workspace must be contiguous, on the cache's device");
+      ptr = t.data_ptr();
+      have = t.nbytes();
+    } else if (bytes) {
+      space = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+      ptr = space.data_ptr();
+      have = bytes;
+    }
     run(index, [&](void *s) {
       return f_evict(&c, &e, weights.data_ptr<float>(), kept.data_ptr<int32_t>(),
-                     left.data_ptr<int32_t>(), s);
+                     left.data_ptr<int32_t>(), ptr, have, s);
     });
     for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(v[2]); ++i)
       if (auto *t = tensor_or_none(PyTuple_GET_ITEM(v[2], i), "the cache's")) written(*t);
     written(weights);
+    if (v[10] != Py_None) written(tensor(v[10], "workspace"));
     PyObject *a = THPVariable_Wrap(std::move(kept)), *z = a ? THPVariable_Wrap(std::move(left)) : nullptr;
     PyObject *both = z ? PyTuple_Pack(2, a, z) : nullptr;
     Py_XDECREF(a);
@@ -740,12 +777,12 @@ PyObject *evict(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
   });
 }
 
-// bind(addresses of the ten entry points, binding._check, stream of a GPU, current GPU,
+// bind(addresses of the eleven entry points, binding._check, stream of a GPU, current GPU,
 //      torch.cuda.device)
 PyObject *bind(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
-  ARGS(14)
-  void *p[10];
-  for (int i = 0; i < 10; ++i) {
+  ARGS(15)
+  void *p[11];
+  for (int i = 0; i < 11; ++i) {
     p[i] = PyLong_AsVoidPtr(v[i]);
     if (PyErr_Occurred()) return nullptr;
   }
@@ -758,11 +795,12 @@ PyObject *bind(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
   f_enter = reinterpret_cast<decltype(f_enter)>(p[6]);
   f_weigh_workspace = reinterpret_cast<decltype(f_weigh_workspace)>(p[7]);
   f_weigh = reinterpret_cast<decltype(f_weigh)>(p[8]);
-  f_evict = reinterpret_cast<decltype(f_evict)>(p[9]);
+  f_evict_workspace = reinterpret_cast<decltype(f_evict_workspace)>(p[9]);
+  f_evict = reinterpret_cast<decltype(f_evict)>(p[10]);
   PyObject **kept[4] = {&g_check, &g_stream, &g_device, &g_on};
   for (int i = 0; i < 4; ++i) {
-    Py_INCREF(v[10 + i]);
-    Py_XSETREF(*kept[i], v[10 + i]);
+    Py_INCREF(v[11 + i]);
+    Py_XSETREF(*kept[i], v[11 + i]);
   }
   Py_RETURN_NONE;
 }
@@ -771,7 +809,8 @@ PyObject *bind(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
 PyMethodDef methods[] = {METHOD(bind),      METHOD(rotary),    METHOD(cache),
                          METHOD(append),    METHOD(read),      METHOD(attention_workspace_bytes),
                          METHOD(attention), METHOD(norm_rotary), METHOD(enter),
-                         METHOD(weigh_workspace_bytes), METHOD(weigh), METHOD(evict),
+                         METHOD(weigh_workspace_bytes), METHOD(weigh),
+                         METHOD(evict_workspace_bytes), METHOD(evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv", "Argument checks of kv.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

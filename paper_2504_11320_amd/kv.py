@@ -63,7 +63,8 @@ def _lib():
         L.wait_kv_enter.argtypes = [s, s, s, i32, s, s, p, i64, s, s, s, p]
         L.wait_kv_weigh_workspace_bytes.argtypes = [s, s, C.POINTER(C.c_size_t)]
         L.wait_kv_weigh.argtypes = [s, s, s, p, p, i32, p, C.c_size_t, p]
-        L.wait_kv_evict.argtypes = [s, s, p, p, p, p]
+        L.wait_kv_evict_workspace_bytes.argtypes = [s, s, C.POINTER(C.c_size_t)]
+        L.wait_kv_evict.argtypes = [s, s, p, p, p, p, C.c_size_t, p]
         _fn = L
     return _fn
 
@@ -83,7 +84,8 @@ def _native():
         native.bind(*(C.cast(f, C.c_void_p).value for f in (
             L.wait_kv_rotary, L.wait_kv_append, L.wait_kv_read,
             L.wait_kv_attention_workspace_bytes, L.wait_kv_attention, L.wait_kv_norm_rotary,
-            L.wait_kv_enter, L.wait_kv_weigh_workspace_bytes, L.wait_kv_weigh, L.wait_kv_evict)),
+            L.wait_kv_enter, L.wait_kv_weigh_workspace_bytes, L.wait_kv_weigh,
+            L.wait_kv_evict_workspace_bytes, L.wait_kv_evict)),
             B._check, stream, current, torch.cuda.device)
         _kv = native
     return _kv
@@ -325,7 +327,7 @@ def weigh_workspace_bytes(q: torch.Tensor, cache: Cache, pages: torch.Tensor, st
 
 def evict(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, weights: torch.Tensor, *,
           keep: int, recent: int = 0, to: Optional[torch.Tensor] = None,
-          max_kv_len: Optional[int] = None) -> tuple:
+          max_kv_len: Optional[int] = None, workspace: Optional[torch.Tensor] = None) -> tuple:
     """Takes every request back to ``keep`` keys: of one that has more, each KV
     head keeps the last ``recent`` and, of the others, those with the largest
     ``weights`` (equal ones: the lower index; NaN is larger than all else).  Kept
@@ -340,6 +342,15 @@ def evict(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, weights: tor
     (kept [requests, kv_heads, keep] int32, the indices of the kept keys, -1
     behind a request's last; new lengths [requests], min(kv_lens, keep)).  Attention over the
     kept rows must not be windowed by positions: their indices are new ones, and
-    differ from head to head."""
+    differ from head to head.  ``workspace`` (a uint8 tensor of
+    ``evict_workspace_bytes``) is taken from PyTorch where it is not given."""
     return _native().evict(cache._c, cache._index, cache._tensors, pages, kv_lens, weights, keep,
-                           recent, to, max_kv_len)
+                           recent, to, max_kv_len, workspace)
+
+
+def evict_workspace_bytes(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, *, keep: int,
+                          recent: int = 0, to: Optional[torch.Tensor] = None,
+                          max_kv_len: Optional[int] = None) -> int:
+    """Bytes that ``evict`` takes as its workspace for these shapes."""
+    return _native().evict_workspace_bytes(cache._c, cache._index, pages, kv_lens, keep, recent, to,
+                                           max_kv_len)

@@ -16,7 +16,8 @@ FAKE = 1 << 40   # never dereferenced: the checks come first
 
 @pytest.mark.parametrize("header,names", [
     ("wait_kv_norm.h", ["wait_kv_enter", "wait_kv_norm_rotary"]),
-    ("wait_kv_budget.h", ["wait_kv_evict", "wait_kv_weigh", "wait_kv_weigh_workspace_bytes"])])
+    ("wait_kv_budget.h", ["wait_kv_evict", "wait_kv_evict_workspace_bytes", "wait_kv_weigh",
+                          "wait_kv_weigh_workspace_bytes"])])
 def test_library_exports_header_symbols(header, names):
     src = open(os.path.join(ROOT, "include", header)).read()
     assert sorted(set(re.findall(r"^int (wait_kv_\w+)\s*\(", src, re.M))) == names
@@ -137,7 +138,7 @@ def test_evict_refusals():
     L = kv._lib()
 
     def call(c=None, e=None, w=FAKE, kept=FAKE << 2, left=FAKE << 3):
-        return L.wait_kv_evict(c or cache(), e or eviction(), w, kept, left, None)
+        return L.wait_kv_evict(c or cache(), e or eviction(), w, kept, left, None, 0, None)
 
     for kw in (dict(c=cache(pages=0)), dict(e=eviction(n_seq=-1)), dict(e=eviction(keep=0)),
                dict(e=eviction(keep=-3)), dict(e=eviction(recent=-1)),
@@ -152,6 +153,7 @@ def test_evict_refusals():
                dict(c=cache(dim=8))):
         refused(call(**kw), B.WS_EUNSUPPORTED)
     assert call(e=eviction(n_seq=0)) == B.WS_OK
+    refused(call(e=eviction(table_cols=1 << 10, max_kv_len=10000)), B.WS_EWORKSPACE)
 
 
 def small(dtype=torch.bfloat16):
@@ -262,6 +264,19 @@ def test_weigh_workspace_is_the_librarys():
         assert n >= 0 and n % 4 == 0
     with pytest.raises(B.WaitSimError):
         kv.weigh_workspace_bytes(t["q"], small(), t["pages"], t["starts"], t["lens"], window=-1)
+
+
+def test_evict_workspace():
+    """None for short requests, by the bound; as the library says."""
+    c = kv.Cache.empty(4096, 16, 2, 64, device="cpu")
+    pages, lens = torch.zeros(3, 1024, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    assert kv.evict_workspace_bytes(c, pages, lens, keep=5, max_kv_len=2048) == 0
+    a = kv.evict_workspace_bytes(c, pages, lens, keep=5, max_kv_len=2049)
+    b = kv.evict_workspace_bytes(c, pages, lens, keep=5)
+    assert 0 < a < b and b == 4 * a   # 4096 keys a part
+    assert kv.evict_workspace_bytes(c, pages[:0], lens[:0], keep=5) == 0
+    with pytest.raises((ValueError, B.WaitSimError)):
+        kv.evict_workspace_bytes(c, pages, lens, keep=5, max_kv_len=-1)
 
 
 def test_the_oracles_choice():
