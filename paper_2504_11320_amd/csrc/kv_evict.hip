@@ -2,8 +2,8 @@
 // KV head are found, then their rows move.
 //
 // Weights are compared as whole numbers of the same order.  Up to 2048 keys, a
-// wave holds them in registers and halves the range that the smallest kept one
-// lies in until as many are above as may stay.  More keys are split over
+// workgroup holds them in registers and narrows the range that the smallest kept
+// one lies in until as many are above as may stay.  More keys are split over
 // workgroups, and that number is found digit by digit: a histogram of the next
 // digit of those that share the digits so far, one launch each.
 #include <algorithm>
@@ -82,84 +82,144 @@ struct Pair {
   }
 };
 
-// ------------------------------------------------- up to 2048 keys ------
+// ----------------------------------------------------- a workgroup ------
+//
+// Four waves hold up to 4096 keys: lane l of wave w the keys w 64 R + 64 i + l, R at
+// most 16, in registers.
 
-constexpr int kHeld = 32;  // keys of a lane, at most
-
-// The kept ones of n keys, 0 < need < n <= 64 R: `kept` gets their indices.
-template <int R, class F>
-__device__ __forceinline__ void pick_held(int32_t n, int32_t need, F &&order, int32_t *kept) {
-  const int lane = threadIdx.x & 63;
-  uint32_t x[R];
-#pragma unroll
-  for (int i = 0; i < R; ++i) x[i] = order(min(64 * i + lane, n - 1));
-  uint32_t low = 0xffffffffu, high = 0;
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    low = min(low, x[i]);
-    high = max(high, x[i]);
-    // Behind the last key 0, which is not more than any: it is not counted, and
-    // where it equals the smallest kept number it comes behind all that do.
-    if (64 * i + lane >= n) x[i] = 0;
-  }
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    low = min(low, (uint32_t)__shfl_xor((int)low, m));
-    high = max(high, (uint32_t)__shfl_xor((int)high, m));
-  }
-  // More than `need` numbers are lo or more, up to that many are above hi: the
-  // smallest kept one is in lo .. hi.
-  uint32_t lo = __builtin_amdgcn_readfirstlane(low), hi = __builtin_amdgcn_readfirstlane(high);
-  int32_t left = need;  // of those that equal hi, once that is lo
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2 + 1;  // lo < mid <= hi
-    int32_t c = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) c += __popcll(__ballot(x[i] >= mid));
-    if (c > need) {
-      lo = mid;
-    } else {
-      hi = mid - 1;
-      left = need - c;
-      if (left == 0) break;  // those above hi are the kept ones
-    }
-  }
-  int32_t at = 0;
-  const uint64_t below = (1ull << lane) - 1;
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const uint64_t same = __ballot(x[i] == hi);
-    const bool stays = x[i] > hi || (x[i] == hi && (int32_t)__popcll(same & below) < left);
-    left = max(0, left - (int32_t)__popcll(same));
-    const uint64_t all = __ballot(stays);
-    if (stays) kept[at + __popcll(all & below)] = 64 * i + lane;
-    at += __popcll(all);
-  }
-}
-template <class F>
-__device__ __forceinline__ void pick_held(int32_t n, int32_t need, F &&order, int32_t *kept) {
-  if (n <= 64 * 8)
-    pick_held<8>(n, need, order, kept);
-  else if (n <= 64 * 16)
-    pick_held<16>(n, need, order, kept);
-  else if (n <= 64 * 24)
-    pick_held<24>(n, need, order, kept);
-  else
-    pick_held<kHeld>(n, need, order, kept);
-}
-
-// ------------------------------------------- any number, a workgroup ----
-
-struct Scan {
+struct Shared {
   int32_t count[4][256];
-  int32_t above[4], equal[4];
+  int32_t among[2][4][4];  // [turn][wave]
   uint32_t digit;
   int32_t left;
 };
 
+template <int R>
+struct Held {
+  uint32_t x[R];
+  // The keys from .. to - 1, of up to 256 R; what lies behind them is 0.
+  template <class F>
+  __device__ __forceinline__ void load(int32_t from, int32_t to, F &&order) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) x[i] = order(min(from + key(i), to - 1));
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (from + key(i) >= to) x[i] = 0;
+  }
+  static __device__ __forceinline__ int32_t key(int i) {
+    return (threadIdx.x >> 6) * 64 * R + 64 * i + (threadIdx.x & 63);
+  }
+};
+
+// Writes the kept ones of keys from .. to - 1 behind kept[0 .. at - 1]: larger than
+// `least`, or among the first `left` that equal it.  at and left are then what the
+// keys behind find.
+template <int R>
+__device__ __forceinline__ void write_kept(Shared &sh, const Held<R> &k, int32_t from, int32_t to,
+                                           uint32_t least, int32_t *left, int32_t *at,
+                                           int32_t *kept) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int32_t more = 0, same = 0;
+  auto there = [&](int i) { return from + k.key(i) < to; };
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    more += (int32_t)__popcll(__ballot(there(i) && k.x[i] > least));
+    same += (int32_t)__popcll(__ballot(there(i) && k.x[i] == least));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    sh.among[0][wave][0] = more;
+    sh.among[0][wave][1] = same;
+  }
+  __syncthreads();
+  int32_t my_left = *left, my_at = *at, all_more = 0, all_same = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w == wave) {
+      my_at += all_more + min(all_same, *left);
+      my_left = max(0, *left - all_same);
+    }
+    all_more += sh.among[0][w][0];
+    all_same += sh.among[0][w][1];
+  }
+  *at += all_more + min(all_same, *left);
+  *left = max(0, *left - all_same);
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const uint64_t ties = __ballot(there(i) && k.x[i] == least);
+    const bool stays = there(i) && (k.x[i] > least || (k.x[i] == least &&
+                                                       (int32_t)__popcll(ties & below) < my_left));
+    my_left = max(0, my_left - (int32_t)__popcll(ties));
+    const uint64_t all = __ballot(stays);
+    if (stays) kept[my_at + (int32_t)__popcll(all & below)] = from + k.key(i);
+    my_at += (int32_t)__popcll(all);
+  }
+}
+
+// The kept ones of n <= 256 R keys, 0 < need < n.  More than `need` numbers are lo
+// or more, up to that many are above hi: the smallest kept one is in lo .. hi, of
+// which each turn leaves a quarter.
+template <int R, class F>
+__device__ __forceinline__ void pick_held(Shared &sh, int32_t n, int32_t need, F &&order,
+                                          int32_t *kept) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Held<R> k;
+  k.load(0, n, order);
+  uint32_t lo = 0, hi = 0xffffffffu;
+  int32_t left = need;  // of those that equal hi, once that is lo
+  for (int turn = 0; lo < hi && left > 0; turn ^= 1) {
+    const uint32_t quarter = (hi - lo) / 4;
+    uint32_t mid[3];  // lo < mid <= hi
+    int32_t c[3] = {0, 0, 0};
+#pragma unroll
+    for (int m = 0; m < 3; ++m) {
+      mid[m] = lo + 1 + (m + 1) * quarter;
+#pragma unroll
+      for (int i = 0; i < R; ++i) c[m] += (int32_t)__popcll(__ballot(k.x[i] >= mid[m]));
+    }
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int m = 0; m < 3; ++m) sh.among[turn][wave][m] = c[m];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < 3; ++m)
+      c[m] = __builtin_amdgcn_readfirstlane(sh.among[turn][0][m] + sh.among[turn][1][m] +
+                                            sh.among[turn][2][m] + sh.among[turn][3][m]);
+#pragma unroll
+    for (int m = 2; m >= 0; --m)
+      if (c[m] <= need) {
+        hi = mid[m] - 1;
+        left = need - c[m];
+      }
+#pragma unroll
+    for (int m = 0; m < 3; ++m)
+      if (c[m] > need) lo = mid[m];
+  }
+  int32_t at = 0;
+  write_kept(sh, k, 0, n, hi, &left, &at, kept);
+}
+template <class F>
+__device__ __forceinline__ void pick_held(Shared &sh, int32_t n, int32_t need, F &&order,
+                                          int32_t *kept) {
+  if (n <= 512)
+    pick_held<2>(sh, n, need, order, kept);
+  else if (n <= 1024)
+    pick_held<4>(sh, n, need, order, kept);
+  else if (n <= 1536)
+    pick_held<6>(sh, n, need, order, kept);
+  else
+    pick_held<8>(sh, n, need, order, kept);
+}
+
+constexpr int kHeld = 2048;  // keys of pick_held, at most
+constexpr int kPart = 4096;  // keys that are counted at a time
+
 // Of the counts of 256 digits, the digit that the left-th largest has, and how many
 // of those with it stay: sh.digit, sh.left.
-__device__ __forceinline__ void find_digit(Scan &sh, int32_t left) {
+__device__ __forceinline__ void find_digit(Shared &sh, int32_t left) {
   if (threadIdx.x < 64) {  // four digits a lane, the largest in lane 0
     const int lane = threadIdx.x;
     int32_t c[4], mine = 0;
@@ -183,89 +243,52 @@ __device__ __forceinline__ void find_digit(Scan &sh, int32_t left) {
   __syncthreads();
 }
 
-// Counts of a digit of the keys from .. to - 1 that share the digits above it, one
-// array a wave, added up in the first.
-template <class F>
-__device__ __forceinline__ void count_digits(Scan &sh, int32_t from, int32_t to, uint32_t least,
-                                             int shift, F &&order) {
+// Adds to the counts of a digit, one array a wave, those of the keys that share the
+// digits above it.
+__device__ __forceinline__ void count_held(Shared &sh, const Held<16> &k, int32_t from, int32_t to,
+                                           uint32_t least, int shift) {
   const int wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (from + k.key(i) < to && (shift == 24 || (k.x[i] ^ least) >> (shift + 8) == 0))
+      atomicAdd(&sh.count[wave][k.x[i] >> shift & 255], 1);
+}
+__device__ __forceinline__ void clear_counts(Shared &sh) {
   for (int i = threadIdx.x; i < 1024; i += 256) sh.count[0][i] = 0;
   __syncthreads();
-  constexpr int ahead = 4;
-  for (int32_t j0 = from; j0 < to; j0 += 256 * ahead) {
-    uint32_t x[ahead];
-#pragma unroll
-    for (int i = 0; i < ahead; ++i) x[i] = order(min(j0 + i * 256 + (int32_t)threadIdx.x, to - 1));
-#pragma unroll
-    for (int i = 0; i < ahead; ++i) {
-      const bool is = j0 + i * 256 + (int32_t)threadIdx.x < to;
-      if (is && (shift == 24 || (x[i] ^ least) >> (shift + 8) == 0))
-        atomicAdd(&sh.count[wave][x[i] >> shift & 255], 1);
-    }
-  }
+}
+// All waves' in the first array.
+__device__ __forceinline__ void add_counts(Shared &sh) {
   __syncthreads();
   const int t = threadIdx.x;
   sh.count[0][t] += sh.count[1][t] + sh.count[2][t] + sh.count[3][t];
   __syncthreads();
 }
 
-// The kept ones of the keys from .. to - 1 go to kept[above + min(equal, left)] and
-// on: larger than least, or among the first `left` that equal it, `equal` of
-// which lie before.
-template <class F>
-__device__ __forceinline__ void write_kept(Scan &sh, int32_t from, int32_t to, uint32_t least,
-                                           int32_t left, int32_t above, int32_t equal, F &&order,
-                                           int32_t *kept) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // each wave takes keys that follow one another
-  const int32_t each = ((to - from + 3) / 4 + 63) / 64 * 64;
-  const int32_t first = min(from + wave * each, to), last = min(first + each, to);
-  int32_t more = 0, same = 0;
-  for (int32_t j0 = first; j0 < last; j0 += 64) {
-    const int32_t j = j0 + lane;
-    const uint32_t x = order(min(j, to - 1));
-    more += __popcll(__ballot(j < last && x > least));
-    same += __popcll(__ballot(j < last && x == least));
-  }
-  if (lane == 0) {
-    sh.above[wave] = more;
-    sh.equal[wave] = same;
-  }
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) {
-    above += sh.above[w];
-    equal += sh.equal[w];
-  }
-  int32_t at = above + min(equal, left);
-  const uint64_t below = (1ull << lane) - 1;
-  for (int32_t j0 = first; j0 < last; j0 += 64) {
-    const int32_t j = j0 + lane;
-    const uint32_t x = order(min(j, to - 1));
-    const uint64_t ties = __ballot(j < last && x == least);
-    const bool stays =
-        j < last && (x > least || (x == least && equal + (int32_t)__popcll(ties & below) < left));
-    const uint64_t all = __ballot(stays);
-    if (stays) kept[at + __popcll(all & below)] = j;
-    at += __popcll(all);
-    equal += __popcll(ties);
-  }
-}
-
 // The kept ones of a request longer than its launch was laid out for, by one
 // workgroup.
 template <class F>
-__device__ __forceinline__ void pick_any(Scan &sh, int32_t n, int32_t need, F &&order, int32_t *kept) {
+__device__ __forceinline__ void pick_any(Shared &sh, int32_t n, int32_t need, F &&order,
+                                         int32_t *kept) {
   uint32_t least = 0;
-  int32_t left = need;
+  int32_t left = need, at = 0;
+  Held<16> k;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    count_digits(sh, 0, n, least, shift, order);
+    clear_counts(sh);
+    for (int32_t from = 0; from < n; from += kPart) {
+      k.load(from, n, order);
+      count_held(sh, k, from, n, least, shift);
+    }
+    add_counts(sh);
     find_digit(sh, left);
     least |= sh.digit << shift;
     left = sh.left;
     __syncthreads();
   }
-  write_kept(sh, 0, n, least, left, 0, 0, order, kept);
+  for (int32_t from = 0; from < n; from += kPart) {
+    k.load(from, n, order);
+    write_kept(sh, k, from, n, least, &left, &at, kept);
+  }
 }
 
 // ------------------------------------------------------ many keys -------
@@ -280,12 +303,12 @@ __device__ __forceinline__ Range part_of(const Args &a, int32_t part, int32_t n)
 
 // The digit that the counts of all parts give; what this part knows behind it;
 // `equal` gets how many of the parts before share it.
-__device__ __forceinline__ Found next_digit(Scan &sh, const Args &a, int32_t pair, int32_t part,
+__device__ __forceinline__ Found next_digit(Shared &sh, const Args &a, int32_t pair, int32_t part,
                                             int digit, Found f, int32_t *equal) {
   const int t = threadIdx.x;
   const int32_t *c = a.counts + (((int64_t)digit * (gridDim.x / a.parts) + pair) * a.parts) * 256 + t;
   int32_t all = 0, before = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (int32_t q = 0; q < a.parts; ++q) {
     const int32_t x = c[q * 256];
     all += x;
@@ -298,9 +321,9 @@ __device__ __forceinline__ Found next_digit(Scan &sh, const Args &a, int32_t pai
   const uint32_t d = sh.digit;
   int32_t above = (uint32_t)t > d ? before : 0;
   for (int m = 1; m < 64; m *= 2) above += __shfl_xor(above, m);
-  if ((t & 63) == 0) sh.above[t >> 6] = above;
+  if ((t & 63) == 0) sh.among[0][t >> 6][0] = above;
   __syncthreads();
-  f.above += sh.above[0] + sh.above[1] + sh.above[2] + sh.above[3];
+  f.above += sh.among[0][0][0] + sh.among[0][1][0] + sh.among[0][2][0] + sh.among[0][3][0];
   f.least |= d << (24 - 8 * digit);
   f.left = sh.left;
   *equal = sh.count[1][d];
@@ -309,10 +332,9 @@ __device__ __forceinline__ Found next_digit(Scan &sh, const Args &a, int32_t pai
 }
 
 // Launch number `digit` counts that digit, once the ones before are known; the one
-// behind the last digit writes the kept keys.  131,072 keys of 8 heads: five
-// launches of 2 to 4 us, 310 us by one workgroup a head.
+// behind the last digit writes the kept keys.
 __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
-  __shared__ Scan sh;
+  __shared__ Shared sh;
   const int32_t part = blockIdx.x % a.parts, pair = blockIdx.x / a.parts;
   const Pair p(a, pair);
   int32_t *kept = a.kept + (int64_t)pair * a.keep;
@@ -324,22 +346,36 @@ __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
         kept[d] = p.simply(a, d);
     return;
   }
+  // the keys are asked for before the digit is known
+  const Range r = part_of(a, part, p.n);
+  auto order = [&](int32_t j) { return p.order(a, j); };
+  Held<16> k;
+  if (r.lo < r.hi) k.load(r.lo, min(r.hi, r.lo + kPart), order);
   Found f = {0, p.need, 0, 0};
   int32_t equal = 0;
   if (digit > 0) {
     if (digit > 1) f = a.found[blockIdx.x];
     f = next_digit(sh, a, pair, part, digit - 1, f, &equal);
   }
-  const Range r = part_of(a, part, p.n);
-  auto order = [&](int32_t j) { return p.order(a, j); };
   if (digit < 4) {
     if (digit > 0 && threadIdx.x == 0) a.found[blockIdx.x] = f;
-    count_digits(sh, r.lo, r.hi, f.least, 24 - 8 * digit, order);
+    clear_counts(sh);
+    for (int32_t from = r.lo; from < r.hi; from += kPart) {
+      const int32_t to = min(r.hi, from + kPart);
+      if (from > r.lo) k.load(from, to, order);
+      count_held(sh, k, from, to, f.least, 24 - 8 * digit);
+    }
+    add_counts(sh);
     a.counts[((int64_t)digit * gridDim.x + blockIdx.x) * 256 + threadIdx.x] =
         sh.count[0][threadIdx.x];
     return;
   }
-  if (r.lo < r.hi) write_kept(sh, r.lo, r.hi, f.least, f.left, f.above, equal, order, kept);
+  int32_t left = max(0, f.left - equal), at = f.above + min(equal, f.left);
+  for (int32_t from = r.lo; from < r.hi; from += kPart) {
+    const int32_t to = min(r.hi, from + kPart);
+    if (from > r.lo) k.load(from, to, order);
+    write_kept(sh, k, from, to, f.least, &left, &at, kept);
+  }
   for (int32_t d = part * 256 + threadIdx.x; d < a.recent; d += a.parts * 256)
     kept[p.need + d] = p.n + d;
 }
@@ -410,19 +446,19 @@ __global__ void __launch_bounds__(256) move_kernel(Args a) {
 // for itself, which takes less than another launch.
 template <int C>
 __global__ void __launch_bounds__(256) pick_kernel(Args a) {
-  __shared__ Scan sh;
-  __shared__ int32_t list[64 * kHeld];
+  __shared__ Shared sh;
+  __shared__ int32_t list[kHeld];
   const int32_t pair = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
   const Pair p(a, pair);
   int32_t *kept = a.kept + (int64_t)pair * a.keep;
   if (p.h == 0 && block == 0 && threadIdx.x == 0) a.new_lens[pair / a.kv_heads] = min(p.m, a.keep);
-  const bool simple = p.simple(a), held = p.n <= 64 * kHeld;
+  const bool simple = p.simple(a), held = p.n <= kHeld;
   auto order = [&](int32_t j) { return p.order(a, j); };
   if (!simple) {
     if (!held)  // the same list by each of the workgroups
       pick_any(sh, p.n, p.need, order, kept);
-    else if (threadIdx.x < 64)
-      pick_held(p.n, p.need, order, list);
+    else
+      pick_held(sh, p.n, p.need, order, list);
     __syncthreads();
   }
   auto key_of = [&](int32_t d) {
@@ -503,12 +539,10 @@ __global__ void __launch_bounds__(256) close_up_kernel(Args a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-constexpr int64_t kPart = 4096;  // keys that a workgroup counts
-
 // The parts that a request's keys are counted in; 0 where they are not.
 int32_t parts_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
   const int64_t longest = std::min<int64_t>(e.max_kv_len, (int64_t)e.table_cols * c.page_size);
-  return longest <= 64 * kHeld ? 0 : (int32_t)ceil_div(longest, kPart);
+  return longest <= kHeld ? 0 : (int32_t)ceil_div(longest, kPart);
 }
 int64_t bytes_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
   return (int64_t)e.n_seq * c.kv_heads * parts_of(c, e) * (4 * 256 * 4 + (int64_t)sizeof(Found));
