@@ -6,6 +6,7 @@
 // partners in the rotation, so that norm and rotation need no more than one sum
 // over the lanes; an 8-bit cache takes one more, the row's largest magnitude.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv_rows.h"
 #include "wait_kv_norm.h"
@@ -61,6 +62,68 @@ __device__ __forceinline__ void load_weights(const Side &s, int32_t h, int32_t d
   }
 }
 
+// Weights asked for and not yet waited for: VEC of 32 bits, or of 16 in the first
+// half of the words.  (As vectors: arrays end in memory here.)
+template <int VEC>
+struct AskedWeights {
+  u32x4 a, b;
+  __device__ __forceinline__ AskedWeights(const void *w, int64_t at, bool wide) {
+    const uint32_t *p = (const uint32_t *)w + at;
+    const uint16_t *q = (const uint16_t *)w + at;
+    a = b = u32x4{0, 0, 0, 0};
+    if constexpr (VEC == 8) {
+      a = *reinterpret_cast<const u32x4 *>(wide ? (const void *)p : q);
+      if (wide) b = *reinterpret_cast<const u32x4 *>(p + 4);
+    } else if constexpr (VEC == 4) {
+      if (wide) {
+        a = *reinterpret_cast<const u32x4 *>(p);
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(q);
+        a = u32x4{x[0], x[1], 0, 0};
+      }
+    } else {
+      if (wide) {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+        a = u32x4{x[0], x[1], 0, 0};
+      } else {
+        a[0] = *reinterpret_cast<const uint32_t *>(q);
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int type, float (&w)[VEC]) const {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const uint32_t full = i < 4 ? a[i & 3] : b[i & 3];
+      const uint16_t half = (uint16_t)(a[i / 2] >> (16 * (i & 1)));
+      const float x = type == WS_KV_BF16 ? Bf16::get(half) : Fp16::get(half);
+      w[i] = type == WS_KV_FP32 ? __uint_as_float(full) : x;
+    }
+  }
+};
+
+// f over the lanes of a group, up to 16 without leaving the registers: neighbours,
+// pairs, then mirrored halves, whose lanes hold the same by then.
+template <class F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t x, int lanes, F &&f) {
+  auto with = [&](auto control) {
+    x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(control)::value, 0xf, 0xf, true));
+  };
+  if (lanes > 1) with(std::integral_constant<int, 0xb1>{});    // 1 0 3 2
+  if (lanes > 2) with(std::integral_constant<int, 0x4e>{});    // 2 3 0 1
+  if (lanes > 4) with(std::integral_constant<int, 0x141>{});   // 7 .. 0
+  if (lanes > 8) with(std::integral_constant<int, 0x140>{});   // 15 .. 0
+  for (int m = 16; m < lanes; m *= 2) x = f(x, (uint32_t)__shfl_xor((int)x, m));
+  return x;
+}
+__device__ __forceinline__ float sum_over(float x, int lanes) {
+  return __uint_as_float(over_lanes(__float_as_uint(x), lanes, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+__device__ __forceinline__ uint32_t max_over(uint32_t x, int lanes) {
+  return over_lanes(x, lanes, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+
 // Of a pair of chunks.
 template <int VEC>
 struct Pair {
@@ -87,7 +150,9 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
     is_k = !is_v;
     if (is_v) unit -= a.kv_groups;
   }
-  const Side &s = is_k ? a.k : is_v ? a.v : a.q;
+  Side s = a.q;  // by value: the arguments are not read through a pointer
+  if (is_k) s = a.k;
+  if (is_v) s = a.v;
   const int32_t heads = is_k || is_v ? a.kv_heads : a.heads;
   const int32_t h0 = unit * HPT;
   const int32_t part = a.turn.part, half = part / 2;
@@ -121,11 +186,11 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
     load_raw<T, VEC, acc>(x + h * s.xh + d0, x0[i]);
     load_raw<T, VEC, acc>(x + h * s.xh + d1, x1[i]);
   }
-  Pair<VEC> w;
-  if (s.normed) {
-    load_weights<VEC>(s, h0, d0, w.u);
-    load_weights<VEC>(s, h0, d1, w.w);
-  }
+  // (of a side without weights something that is there, and is not used)
+  const void *weights = s.w ? s.w : s.x;
+  const bool wide = s.w && s.w_type == WS_KV_FP32;
+  const AskedWeights<VEC> w0(weights, s.w ? h0 * s.wh + d0 : 0, wide);
+  const AskedWeights<VEC> w1(weights, s.w ? h0 * s.wh + d1 : 0, wide);
   all_asked(position);
   // angles of the chunks: the same ones where they are partners
   constexpr int NC = INTER ? (VEC + 1) / 2 : VEC;
@@ -145,10 +210,36 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
   }
   const bool stored = TYPE == kNone || !(is_k || is_v) || (slot >= 0 && slot < a.n_slots);
   if (!stored) return;
+  // the heads' sums, one beside the other
+  float r[HPT];
+  Pair<VEC> w;
+  if (s.normed) {
+#pragma unroll
+    for (int i = 0; i < HPT; ++i) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float u = T::get(x0[i][e]), v = T::get(x1[i][e]);
+        sum = __builtin_fmaf(u, u, sum);
+        sum = __builtin_fmaf(v, v, sum);
+      }
+      r[i] = live ? sum : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < HPT; ++i) r[i] = sum_over(r[i], lanes);
+#pragma unroll
+    for (int i = 0; i < HPT; ++i) r[i] = rsqrtf(r[i] / (float)a.dim + s.eps);
+    w0.get(s.w_type, w.u);
+    w1.get(s.w_type, w.w);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      w.u[e] = s.w ? w.u[e] : 1.0f;
+      w.w[e] = s.w ? w.w[e] : 1.0f;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < HPT; ++i) {
     const int32_t h = h0 + i;
-    if (h >= heads) break;
     Pair<VEC> y;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
@@ -156,20 +247,14 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
       y.w[e] = T::get(x1[i][e]);
     }
     if (s.normed) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sum += y.u[e] * y.u[e] + y.w[e] * y.w[e];
-      if (!live) sum = 0.0f;
-      for (int m = 1; m < lanes; m *= 2) sum += __shfl_xor(sum, m);
-      const float r = rsqrtf(sum / (float)a.dim + s.eps);
       if (i > 0 && s.wh) {
-        load_weights<VEC>(s, h, d0, w.u);
-        load_weights<VEC>(s, h, d1, w.w);
+        load_weights<VEC>(s, min(h, heads - 1), d0, w.u);
+        load_weights<VEC>(s, min(h, heads - 1), d1, w.w);
       }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        y.u[e] = y.u[e] * r * w.u[e];
-        y.w[e] = y.w[e] * r * w.w[e];
+        y.u[e] = y.u[e] * r[i] * w.u[e];
+        y.w[e] = y.w[e] * r[i] * w.w[e];
       }
     }
     if constexpr (INTER) {
@@ -198,11 +283,12 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
       }
     }
     if (TYPE == kNone || !(is_k || is_v)) {
-      if (!live) continue;
+      if (!live || h >= heads) continue;
       raw *o = (raw *)a.out + (int64_t)token * a.ot + h * a.oh;
       store_n<T, VEC, acc, STREAM>(o + d0, y.u);
       store_n<T, VEC, acc, STREAM>(o + d1, y.w);
     } else if constexpr (TYPE != kNone) {
+      if (h >= heads) continue;
       const int64_t page = slot >> a.page_shift, off = slot & ((1 << a.page_shift) - 1);
       const int64_t row = ((page * a.kv_heads + h) << a.page_shift) + off;
       void *base = is_k ? a.ck : a.cv;
@@ -216,7 +302,7 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = max(top, max(magnitude(y.u[e]), magnitude(y.w[e])));
-        for (int m = 1; m < lanes; m *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        top = max_over(top, lanes);
         const Coding<TYPE> code(top);
         uint8_t *to = (uint8_t *)base + row * a.dim;
         *reinterpret_cast<u32x2 *>(to + d0) = code.codes(y.u);
