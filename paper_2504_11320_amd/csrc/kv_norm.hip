@@ -130,8 +130,7 @@ struct Pair {
   float u[VEC], w[VEC];
 };
 
-// HPT heads of a token for each group of lanes; a token's groups are those of its
-// queries, its keys, its values.  Everything is asked for before the first use of
+// HPT heads of a token for each group of lanes.  Everything is asked for before the first use of
 // any of it, the position first, which the angles wait for.
 template <class T, int TYPE, int VEC, bool INTER, int HPT, bool STREAM>
 __global__ void __launch_bounds__(256) norm_kernel(Args a) {
@@ -139,17 +138,16 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
   constexpr int acc = VEC < kWide<T> ? VEC : kWide<T>;
   const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1);
   const uint32_t id = blockIdx.x * (256u >> a.lane_bits) + (threadIdx.x >> a.lane_bits);
-  const uint32_t units = (uint32_t)a.q_groups + (TYPE == kNone ? 0 : 2 * a.kv_groups);
-  const uint32_t token = id / units;
-  int32_t unit = (int32_t)(id - token * units);
-  if (token >= a.n) return;  // the lanes of a group end together
-  bool is_k = false, is_v = false;
-  if (TYPE != kNone && unit >= a.q_groups) {
-    unit -= a.q_groups;
-    is_v = unit >= a.kv_groups;
-    is_k = !is_v;
-    if (is_v) unit -= a.kv_groups;
-  }
+  // all queries, then all keys, then all values: a wave has rows of one kind
+  const uint32_t queries = (uint32_t)a.n * (uint32_t)a.q_groups;
+  const uint32_t keys = TYPE == kNone ? 0 : (uint32_t)a.n * (uint32_t)a.kv_groups;
+  if (id >= queries + 2 * keys) return;  // the lanes of a group end together
+  const bool is_k = TYPE != kNone && id >= queries && id < queries + keys;
+  const bool is_v = TYPE != kNone && id >= queries + keys;
+  const uint32_t nth = id - (is_v ? queries + keys : is_k ? queries : 0);
+  const uint32_t groups = is_k || is_v ? a.kv_groups : a.q_groups;
+  const uint32_t token = nth / groups;
+  const int32_t unit = (int32_t)(nth - token * groups);
   Side s = a.q;  // by value: the arguments are not read through a pointer
   if (is_k) s = a.k;
   if (is_v) s = a.v;
