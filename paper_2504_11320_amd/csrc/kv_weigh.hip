@@ -33,7 +33,7 @@ struct Args {
   float scale;  // times log2(e)
   int32_t causal, window, accumulate;
   // what the launch is laid out for
-  int32_t few_parts;     // workgroups of a request and head, of few rows
+  int32_t few_parts;     // waves of a request and head, of few rows
   int32_t both;          // requests of more than 16 rows are the many-rows blocks'
   int32_t tiles, parts;  // of a request's keys and of its rows, of many rows
   float *sums;           // [part][request][KV head][key]
@@ -111,20 +111,28 @@ struct Few {
   static constexpr int keys = 16 * tiles;
 };
 
+// Launches go round the 8 dies.  Four heads in a row go to one die, whose cache then
+// has the lines that the scales and weights of neighbouring heads share.
+__device__ __forceinline__ int32_t near_pairs(int32_t id, int32_t pairs) {
+  if (id >= pairs / 32 * 32) return id;
+  return (id & ~31) | (id & 7) << 2 | (id >> 3 & 3);
+}
+
 template <int TYPE, bool BF, int D>
-__device__ __forceinline__ void few_rows(const Args &a, int32_t id) {
+__device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a wave
   using F = Few<TYPE, D>;
   constexpr bool CODES = kCodes<TYPE>;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4, mine = lane & (F::keys - 1);
-  const int32_t part = id % a.few_parts, pair = id / a.few_parts;
+  const int32_t pairs = a.n_seq * a.kv_heads;
+  const int32_t part = id / pairs, pair = near_pairs(id % pairs, pairs);
+  if (part >= a.few_parts) return;
   const int32_t h = pair % a.kv_heads, b = pair / a.kv_heads;
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
   if (a.both && rows > kFewRows) return;
-  const int32_t end = min(s.m, a.capacity), step = a.few_parts * 4 * F::keys;
-  int32_t k0 = (part * 4 + wave) * F::keys;
+  const int32_t end = min(s.m, a.capacity), step = a.few_parts * F::keys;
+  int32_t k0 = part * F::keys;
   if (k0 >= end) return;
 
   u32x4 q[F::steps];
@@ -177,7 +185,10 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {
   for (; k0 < end; k0 += step) {
     const bool more = end - k0 > step;
     const int32_t next_at = more ? cache_row(a, next_page, h, k0 + step + mine, end) : kNoRow;
-    if (more) next_page = page_entry(a, b, min(k0 + step, end) + step + mine, end);
+    auto load_next = [&] {
+      next_page = page_entry(a, b, min(k0 + step, end) + step + mine, end);
+      load_keys(next_at, k0 + step + mine);
+    };
     const float factor = CODES ? by * a.scale : a.scale, was = weight;
     const int32_t at_row = row_at;
     row_at = next_at;
@@ -207,7 +218,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {
           }
         }
       }
-      if (final && more) load_keys(next_at, k0 + step + mine);
+      if (final && more) load_next();
       const bool all = every.lo <= r0 && every.hi >= min(r0 + 16, rows);
 #pragma unroll
       for (int t = 0; t < F::tiles; ++t) {
@@ -233,8 +244,14 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {
       sum[t] += __shfl_xor(sum[t], 32);
       if (g == t) own = sum[t];
     }
+    if (rows == 0 && more) load_next();
+    // waited for here: behind the store the wait would be for that too
+#pragma unroll
+    for (int t = 0; t < F::tiles; ++t)
+#pragma unroll
+      for (int i = 0; i < F::kloads; ++i) asm volatile("" : "+v"(kreg[t][i]));
+    asm volatile("" : "+v"(by), "+v"(weight), "+v"(next_page));
     if (at_row != kNoRow && lane < F::keys) a.weights[at_row] = was + own;
-    if (rows == 0 && more) load_keys(next_at, k0 + step + mine);
   }
 }
 
@@ -583,7 +600,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
 }
 
 template <int TYPE, bool BF, int D>
-__global__ void __launch_bounds__(256, 2) few_kernel(Args a) {
+__global__ void __launch_bounds__(64, 2) few_kernel(Args a) {
   few_rows<TYPE, BF, D>(a, blockIdx.x);
 }
 
@@ -593,7 +610,8 @@ __global__ void __launch_bounds__(256, 2) many_kernel(Args a, int32_t many) {
   if ((int32_t)blockIdx.x < many)
     many_rows<TYPE, BF, D>(a, blockIdx.x, smem);
   else
-    few_rows<TYPE, BF, D>(a, blockIdx.x - many);
+    few_rows<TYPE, BF, D>(
+        a, __builtin_amdgcn_readfirstlane((blockIdx.x - many) * 4 + (threadIdx.x >> 6)));
 }
 
 // The parts of a key's sum, in their order.
@@ -668,16 +686,18 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
 template <int TYPE, bool BF, int D>
 int weigh_launch(Args a, const Layout &L, int64_t longest, hipStream_t stream) {
   const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
-  const int64_t turns = ceil_div(longest, 4 * Few<TYPE, D>::keys);
-  a.few_parts = (int32_t)std::max<int64_t>(1, std::min(turns, ceil_div(1024, pairs)));
+  // Of few rows: 64 waves a CU, of 8 KB of keys at a time, if there are so many.
+  const int64_t turns = ceil_div(longest, Few<TYPE, D>::keys);
+  a.few_parts = (int32_t)std::min(turns, ceil_div(16384, pairs));
   const int64_t few = pairs * a.few_parts, many = L.many ? pairs * L.tiles * L.parts : 0;
-  if ((few + many) * 256 >= (int64_t)1 << 32 || few + many >= (int64_t)1 << 31)
+  if (few * 64 + (many + 1) * 256 >= (int64_t)1 << 32 || few + many >= (int64_t)1 << 31)
     return ws_record_failure(WS_EUNSUPPORTED, "weigh: too many workgroups");
   if (!L.many) {
-    few_kernel<TYPE, BF, D><<<dim3((uint32_t)few), 256, 0, stream>>>(a);
+    few_kernel<TYPE, BF, D><<<dim3((uint32_t)few), 64, 0, stream>>>(a);
     return launched();
   }
-  many_kernel<TYPE, BF, D><<<dim3((uint32_t)(few + many)), 256, 0, stream>>>(a, (int32_t)many);
+  many_kernel<TYPE, BF, D>
+      <<<dim3((uint32_t)(many + ceil_div(few, 4))), 256, 0, stream>>>(a, (int32_t)many);
   if (int rc = launched()) return rc;
   if (L.bytes) {
     const int64_t joins = pairs * ceil_div(L.tiles, D == 256 ? 2 : 1);
