@@ -38,6 +38,7 @@ struct Args {
   int32_t parts;     // of a request's keys, that are counted
   int32_t *counts;   // [digit][request][KV head][part][256]
   Found *found;      // [request][KV head][part]
+  uint32_t *orders;  // [request][KV head][part][kPart]: the weights as whole numbers
 };
 
 __device__ __forceinline__ int32_t length_of(const Args &a, int32_t b) {
@@ -78,7 +79,8 @@ struct Pair {
   }
   __device__ __forceinline__ uint32_t order(const Args &a, int32_t j) const {
     const int32_t row = row_of(a, pages, h, j);
-    return row == kNoRow ? 0u : order_of(a.weights[row]);
+    const uint32_t x = order_of(a.weights[max(row, 0)]);  // without a branch, which would wait
+    return row == kNoRow ? 0u : x;
   }
 };
 
@@ -87,8 +89,10 @@ struct Pair {
 // Four waves hold up to 4096 keys: lane l of wave w the keys w 64 R + 64 i + l, R at
 // most 16, in registers.
 
+constexpr int kCopies = 4;  // of the counts, one a wave
+
 struct Shared {
-  int32_t count[4][256];
+  int32_t count[kCopies][256];
   int32_t among[2][4][4];  // [turn][wave]
   uint32_t digit;
   int32_t left;
@@ -105,6 +109,15 @@ struct Held {
 #pragma unroll
     for (int i = 0; i < R; ++i)
       if (from + key(i) >= to) x[i] = 0;
+  }
+  // Those that an earlier launch left, and what lies behind them.
+  __device__ __forceinline__ void load_left(const uint32_t *p) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) x[i] = p[key(i)];
+  }
+  __device__ __forceinline__ void leave(uint32_t *p) const {
+#pragma unroll
+    for (int i = 0; i < R; ++i) p[key(i)] = x[i];
   }
   static __device__ __forceinline__ int32_t key(int i) {
     return (threadIdx.x >> 6) * 64 * R + 64 * i + (threadIdx.x & 63);
@@ -243,25 +256,28 @@ __device__ __forceinline__ void find_digit(Shared &sh, int32_t left) {
   __syncthreads();
 }
 
-// Adds to the counts of a digit, one array a wave, those of the keys that share the
+// Adds to the counts of a digit those of the keys that share the
 // digits above it.
 __device__ __forceinline__ void count_held(Shared &sh, const Held<16> &k, int32_t from, int32_t to,
                                            uint32_t least, int shift) {
-  const int wave = threadIdx.x >> 6;
+  const int copy = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < 16; ++i)
     if (from + k.key(i) < to && (shift == 24 || (k.x[i] ^ least) >> (shift + 8) == 0))
-      atomicAdd(&sh.count[wave][k.x[i] >> shift & 255], 1);
+      atomicAdd(&sh.count[copy][k.x[i] >> shift & 255], 1);
 }
 __device__ __forceinline__ void clear_counts(Shared &sh) {
-  for (int i = threadIdx.x; i < 1024; i += 256) sh.count[0][i] = 0;
+  for (int i = threadIdx.x; i < 256 * kCopies; i += 256) sh.count[0][i] = 0;
   __syncthreads();
 }
-// All waves' in the first array.
+// All of them in the first array.
 __device__ __forceinline__ void add_counts(Shared &sh) {
   __syncthreads();
   const int t = threadIdx.x;
-  sh.count[0][t] += sh.count[1][t] + sh.count[2][t] + sh.count[3][t];
+  int32_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) sum += sh.count[i][t];
+  sh.count[0][t] = sum;
   __syncthreads();
 }
 
@@ -336,6 +352,11 @@ __device__ __forceinline__ Found next_digit(Shared &sh, const Args &a, int32_t p
 __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
   __shared__ Shared sh;
   const int32_t part = blockIdx.x % a.parts, pair = blockIdx.x / a.parts;
+  // asked for before anything is known; the first launch leaves the numbers where
+  // they need no page table
+  uint32_t *left_here = a.orders + (int64_t)blockIdx.x * kPart;
+  Held<16> k;
+  if (digit > 0) k.load_left(left_here);
   const Pair p(a, pair);
   int32_t *kept = a.kept + (int64_t)pair * a.keep;
   if (digit == 4 && p.h == 0 && part == 0 && threadIdx.x == 0)
@@ -346,11 +367,12 @@ __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
         kept[d] = p.simply(a, d);
     return;
   }
-  // the keys are asked for before the digit is known
   const Range r = part_of(a, part, p.n);
   auto order = [&](int32_t j) { return p.order(a, j); };
-  Held<16> k;
-  if (r.lo < r.hi) k.load(r.lo, min(r.hi, r.lo + kPart), order);
+  if (r.lo < r.hi && (digit == 0 || r.hi - r.lo > kPart)) {
+    k.load(r.lo, min(r.hi, r.lo + kPart), order);
+    if (digit == 0 && r.hi - r.lo <= kPart) k.leave(left_here);
+  }
   Found f = {0, p.need, 0, 0};
   int32_t equal = 0;
   if (digit > 0) {
@@ -545,7 +567,8 @@ int32_t parts_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
   return longest <= kHeld ? 0 : (int32_t)ceil_div(longest, kPart);
 }
 int64_t bytes_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
-  return (int64_t)e.n_seq * c.kv_heads * parts_of(c, e) * (4 * 256 * 4 + (int64_t)sizeof(Found));
+  return (int64_t)e.n_seq * c.kv_heads * parts_of(c, e) *
+         (4 * 256 * 4 + (int64_t)sizeof(Found) + kPart * 4);
 }
 
 int check_eviction(const ws_kv_cache *c, const ws_kv_eviction *e) {
@@ -651,6 +674,7 @@ int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, floa
     if (bytes) {
       a.found = (Found *)d_workspace;
       a.counts = (int32_t *)(a.found + pairs * a.parts);
+      a.orders = (uint32_t *)(a.counts + pairs * a.parts * 4 * 256);
     }
     hipStream_t s = (hipStream_t)hip_stream;
     switch (cache->dim * type_bytes(cache->type) / 16) {
