@@ -412,34 +412,32 @@ template <int C, class F>
 __device__ __forceinline__ void move_rows(const Args &a, const Pair &p, const int32_t *to,
                                           int32_t d0, int32_t step, int32_t count, F &&key_of) {
   const int lane = threadIdx.x % C;
+  if (count <= 0) return;
+  // all without branches, in which each load would be waited for
   int32_t from[kRows], at[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    const int32_t d = d0 + i * step;
-    from[i] = at[i] = kNoRow;
-    if (d < count) {
-      from[i] = row_of(a, p.pages, p.h, key_of(d));
-      at[i] = row_of(a, to, p.h, d);
-    }
+    const int32_t d = min(d0 + i * step, count - 1);
+    from[i] = row_of(a, p.pages, p.h, key_of(d));
+    at[i] = row_of(a, to, p.h, d);
   }
   u32x4 x[kRows], y[kRows];
   float s[kRows], t[kRows], w[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    if (from[i] == kNoRow || at[i] == kNoRow) continue;
-    x[i] = *reinterpret_cast<const u32x4 *>(a.k + ((int64_t)from[i] * C + lane) * 16);
-    y[i] = *reinterpret_cast<const u32x4 *>(a.v + ((int64_t)from[i] * C + lane) * 16);
-    if (lane == 0) {
-      w[i] = a.weights[from[i]];
-      if (a.ks) {
-        s[i] = a.ks[from[i]];
-        t[i] = a.vs[from[i]];
-      }
+    if (d0 + i * step >= count || from[i] == kNoRow) at[i] = kNoRow;
+    const int32_t row = max(from[i], 0);
+    x[i] = *reinterpret_cast<const u32x4 *>(a.k + ((int64_t)row * C + lane) * 16);
+    y[i] = *reinterpret_cast<const u32x4 *>(a.v + ((int64_t)row * C + lane) * 16);
+    w[i] = a.weights[row];
+    if (a.ks) {
+      s[i] = a.ks[row];
+      t[i] = a.vs[row];
     }
   }
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    if (from[i] == kNoRow || at[i] == kNoRow) continue;
+    if (at[i] == kNoRow) continue;
     *reinterpret_cast<u32x4 *>(a.k + ((int64_t)at[i] * C + lane) * 16) = x[i];
     *reinterpret_cast<u32x4 *>(a.v + ((int64_t)at[i] * C + lane) * 16) = y[i];
     if (lane == 0) {
@@ -521,25 +519,19 @@ __global__ void __launch_bounds__(256) close_up_kernel(Args a) {
     int32_t from[kRows], at[kRows];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      const int32_t d = d0 + i * groups + threadIdx.x / C;
-      from[i] = at[i] = kNoRow;
-      if (d <= last) {
-        from[i] = row_of(a, pages, h, kept[d]);
-        at[i] = row_of(a, pages, h, d);
-      }
+      const int32_t d = min(d0 + i * groups + (int32_t)threadIdx.x / C, last);
+      from[i] = row_of(a, pages, h, kept[d]);
+      at[i] = row_of(a, pages, h, d);
     }
     u32x4 x[kRows];
     float s[kRows], w[kRows];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      x[i] = u32x4{0, 0, 0, 0};
-      s[i] = w[i] = 0.0f;
-      if (from[i] == kNoRow) continue;
-      x[i] = *reinterpret_cast<const u32x4 *>(rows + ((int64_t)from[i] * C + lane) * 16);
-      if (lane == 0) {
-        if (scales) s[i] = scales[from[i]];
-        if (weights) w[i] = weights[from[i]];
-      }
+      if (d0 + i * groups + (int32_t)threadIdx.x / C > last || from[i] == kNoRow) at[i] = kNoRow;
+      const int32_t row = max(from[i], 0);
+      x[i] = *reinterpret_cast<const u32x4 *>(rows + ((int64_t)row * C + lane) * 16);
+      s[i] = scales ? scales[row] : 0.0f;
+      w[i] = weights ? weights[row] : 0.0f;
     }
     // all of it has arrived, in every wave, before any of it is overwritten
 #pragma unroll
@@ -547,7 +539,7 @@ __global__ void __launch_bounds__(256) close_up_kernel(Args a) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      if (from[i] == kNoRow || at[i] == kNoRow) continue;
+      if (at[i] == kNoRow) continue;
       *reinterpret_cast<u32x4 *>(rows + ((int64_t)at[i] * C + lane) * 16) = x[i];
       if (lane == 0) {
         if (scales) scales[at[i]] = s[i];
