@@ -247,3 +247,42 @@ def test_long_contexts():
     """Keys in many workgroups, tokens in many blocks."""
     run([1, 32], [9000, 5000], 64, 8, 1, 64, torch.int8, max_q_len=32, max_kv_len=9000)
     run([1100], [1100], 16, 4, 1, 64, torch.bfloat16)
+
+
+@pytest.mark.parametrize("cache_dtype", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("dim,heads", [(64, 7), (128, 3), (128, 16), (256, 5), (64, 96)])
+def test_rows_in_parts(cache_dtype, dim, heads):
+    """Few keys for many rows, which several workgroups share; groups that do not
+    fill blocks of rows, and larger ones."""
+    n = 900 if heads < 16 else 260
+    for ql, kl, kw in (([n], [n], {}), ([n // 2], [n // 2 + 300], dict(window=70)),
+                       ([n, 3], [100, 500], dict(causal=False)), ([n], [n], dict(accumulate=False))):
+        run(ql, kl, 16, heads, 1, dim, cache_dtype, **kw)
+
+
+def test_no_tokens():
+    """A batch without tokens leaves weights as they are, or takes its requests' to
+    zero where nothing counts."""
+    c = fill(4, 16, 2, 64, torch.bfloat16, 20)
+    q, lse = torch.zeros(0, 4, 64).bfloat16().cuda(), torch.zeros(0, 4).cuda()
+    pages = torch.tensor([[2, 0]], dtype=torch.int32).cuda()
+    starts, lens = torch.zeros(2, dtype=torch.int32).cuda(), torch.tensor([20], dtype=torch.int32).cuda()
+    w = torch.ones(4, 2, 16).cuda()
+    kv.weigh(q, lse, c, pages, starts, lens, w)
+    assert bool((w == 1).all())
+    kv.weigh(q, lse, c, pages, starts, lens, w, accumulate=False)
+    want = torch.ones(4, 2, 16)
+    want[2], want[0, :, :4] = 0, 0
+    assert torch.equal(w.cpu(), want)
+    none = torch.zeros(0, dtype=torch.int32).cuda()
+    kv.weigh(q, lse, c, pages[:0], starts[:1], none, w)
+    assert torch.equal(w.cpu(), want)
+
+
+def test_written_weights_count_a_version():
+    q, pages, starts, lens, n = batch([1], [20], 16, 2, 64, torch.float16, 21)
+    c = fill(n, 16, 2, 64, torch.float16, 22)
+    w = torch.zeros(n, 2, 16).cuda()
+    before = w._version, c.k._version
+    kv.weigh(q.cuda(), torch.zeros(1, 2).cuda(), c, pages.cuda(), starts.cuda(), lens.cuda(), w)
+    assert (w._version, c.k._version) == (before[0] + 1, before[1])
