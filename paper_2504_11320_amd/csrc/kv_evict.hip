@@ -348,7 +348,9 @@ __device__ __forceinline__ Found next_digit(Shared &sh, const Args &a, int32_t p
 }
 
 // Launch number `digit` counts that digit, once the ones before are known; the one
-// behind the last digit writes the kept keys.
+// behind the last digit writes the kept keys.  131,072 keys of 8 heads: five
+// launches of 6 to 8 us, each a chain of loads, counts and barriers; by one
+// workgroup a head 310 us.
 __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
   __shared__ Shared sh;
   const int32_t part = blockIdx.x % a.parts, pair = blockIdx.x / a.parts;
@@ -463,7 +465,9 @@ __global__ void __launch_bounds__(256) move_kernel(Args a) {
 
 // The kept keys of a request and head that has up to 2048 and, where C is not 0,
 // their rows to other pages: the workgroups that share the rows find the keys each
-// for itself, which takes less than another launch.
+// for itself, which takes less than another launch.  One request of 777 keys to 512,
+// 32 heads of 128 bf16: 9.6 us, against 8.0 and 5.3 in two launches; 128 requests of
+// 513 to 1512 keys to 512, fp8 (1.14 GB moved), 268 us (4.3 TB/s).
 template <int C>
 __global__ void __launch_bounds__(256) pick_kernel(Args a) {
   __shared__ Shared sh;
@@ -502,7 +506,7 @@ __global__ void __launch_bounds__(256) pick_kernel(Args a) {
 // never goes behind its place, so what a step writes lies before what later steps
 // read; within a step everything is read before anything is written.  Columns do
 // not meet, so that few requests can have a workgroup for each four of them: one of
-// 131,072 keys to 16,384, 8 heads of 128 bf16, takes 474 us with whole rows.
+// 131,072 keys to 16,384, 8 heads of 128 bf16, takes 155 us, 474 with whole rows.
 template <int C, int W>
 __global__ void __launch_bounds__(256) close_up_kernel(Args a) {
   constexpr int groups = 256 / W, step = groups * kRows;

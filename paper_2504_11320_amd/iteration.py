@@ -260,7 +260,7 @@ def main(argv=None) -> dict:
     points = measure(Server(shape, most, positions=a.prompt + a.out + 1), batches)
     got = fit(points)
     got["C"] = budget(shape, a.kv_bytes)
-    work = calibrate.stage_work(a.prompt, a.out)
+    work = sum(sum(x) for x in stage_batch(a.prompt, a.out, 1, a.keep))   # a request's, over its stages
     got["boundary_per_s"] = 1000.0 * calibrate.fluid_boundary(work, got["d0"], got["d1"], got["C"])
     got["points"] = points
     got["cache"] = a.cache
