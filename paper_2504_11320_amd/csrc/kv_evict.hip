@@ -560,10 +560,11 @@ __global__ void __launch_bounds__(256) close_up_kernel(Args a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The parts that a request's keys are counted in; 0 where they are not.
+// The parts that a request's keys are counted in; 0 where they are not, or where the
+// last ones alone stay.
 int32_t parts_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
   const int64_t longest = std::min<int64_t>(e.max_kv_len, (int64_t)e.table_cols * c.page_size);
-  return longest <= kHeld ? 0 : (int32_t)ceil_div(longest, kPart);
+  return longest <= kHeld || e.keep == e.recent ? 0 : (int32_t)ceil_div(longest, kPart);
 }
 int64_t bytes_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
   return (int64_t)e.n_seq * c.kv_heads * parts_of(c, e) *
