@@ -35,8 +35,10 @@ struct Args {
   // what the launch is laid out for
   int32_t few_parts;     // waves of a request and head, of few rows
   int32_t both;          // requests of more than 16 rows are the many-rows blocks'
-  int32_t tiles, parts;  // of a request's keys and of its rows, of many rows
-  float *sums;           // [part][request][KV head][key]
+  int32_t tiles;         // of a request's keys, of many rows
+  int32_t part_rows;     // rows of a part; 0: they are not split
+  int32_t numbers;       // of parts: of all requests
+  float *sums;           // [number of a part][KV head][key]
 };
 
 constexpr float kLog2E = 1.44269504088896340736f;
@@ -324,6 +326,14 @@ __device__ __forceinline__ int row_swizzle(int r) {
   return D == 64 ? (r >> 1) & 7 : r & 15;
 }
 
+// The number of the first part of request b: parts are numbered so that they need
+// no count of those before, and no two requests share one.
+__device__ __forceinline__ int32_t first_part(const Args &a, int32_t b) {
+  if (!a.part_rows) return b;
+  const int32_t at = min(max(a.starts[b], 0), a.n_tokens);
+  return (int32_t)((uint32_t)(at * a.group) / (uint32_t)a.part_rows) + b;  // below 2^31 rows
+}
+
 // Rows [lo, hi) of a part of those that see some key of a workgroup's.
 struct Parts {
   int32_t lo, hi, each, parts;
@@ -337,7 +347,7 @@ __device__ __forceinline__ Parts parts_of(const Args &a, const Seq &s, int32_t t
   p.hi = rows_of_key(a, s, min(k0 + M::keys, end) - 1, rows).hi;
   // a tile that the launch was not laid out for has no room for parts
   const int32_t blocks = p.hi > p.lo ? (p.hi - p.lo + M::rows - 1) / M::rows : 0;
-  const int32_t most = tile < a.tiles ? a.parts : 1;
+  const int32_t most = tile < a.tiles && a.part_rows && rows ? (rows - 1) / a.part_rows + 1 : 1;
   p.each = max(1, (blocks + most - 1) / most) * M::rows;
   p.parts = max(1, (blocks * M::rows + p.each - 1) / p.each);
   return p;
@@ -353,9 +363,11 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hh = lane >> 5, mine = lane & (own - 1);
   // the first keys have most rows, and go first
-  const int32_t pairs = a.n_seq * a.kv_heads;
-  const int32_t pair = id % pairs, part = id / pairs % a.parts;
-  const int32_t h = pair % a.kv_heads, b = pair / a.kv_heads;
+  const int32_t h = id % a.kv_heads, nth = id / a.kv_heads % a.numbers;
+  const int32_t b =
+      a.part_rows ? last_at_most(a, [&](int32_t i) { return first_part(a, i) <= nth; }) : nth;
+  if (b < 0) return;
+  const int32_t part = __builtin_amdgcn_readfirstlane(nth - first_part(a, b));
   const Seq s = get_seq(a, b);
   const int32_t rows = s.n * a.group;
   if (rows <= kFewRows) return;
@@ -363,7 +375,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
   const uint32_t shared = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
   float *const logs = (float *)(smem + 3 * M::side);
 
-  for (int32_t tile = id / pairs / a.parts; tile * M::keys < end; tile += a.tiles) {
+  for (int32_t tile = id / a.kv_heads / a.numbers; tile * M::keys < end; tile += a.tiles) {
     const Parts split = parts_of<TYPE, D>(a, s, tile, end);
     if (part >= split.parts) continue;
     const int32_t lo = split.lo + part * split.each, hi = min(split.hi, lo + split.each);
@@ -605,7 +617,8 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
     }
     const bool has = key < end && lane < own;
     if (split.parts > 1) {
-      if (has) a.sums[((int64_t)part * pairs + pair) * a.tiles * M::keys + key] = total;
+      const int64_t number = first_part(a, b) + part;  // again: registers are short above
+      if (has) a.sums[(number * a.kv_heads + h) * a.tiles * M::keys + key] = total;
     } else if (has && row_at != kNoRow) {
       a.weights[row_at] = had + total;
     }
@@ -643,8 +656,8 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
   if (split.parts == 1) return;
   const int32_t row_at = cache_row(a, page_entry(a, b, key, end), h, key, end);
   if (row_at == kNoRow) return;
-  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads, next = pairs * a.tiles * M::keys;
-  const float *p = a.sums + (int64_t)pair * a.tiles * M::keys + key;
+  const int64_t each_part = (int64_t)a.tiles * M::keys, next = a.kv_heads * each_part;
+  const float *p = a.sums + first_part(a, b) * next + h * each_part + key;
   float sum = 0.0f;
   constexpr int ahead = 16;  // parts under way
   for (int32_t i = 0; i < split.parts; i += ahead) {
@@ -682,7 +695,7 @@ int check_weigh(const ws_kv_cache *c, const ws_kv_batch *b) {
 // How a batch is laid out over workgroups.
 struct Layout {
   bool many;
-  int32_t tiles, parts;
+  int32_t tiles, part_rows, numbers;
   int64_t bytes;
 };
 
@@ -693,7 +706,6 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   const int64_t group = b.heads / c.kv_heads, capacity = (int64_t)b.table_cols * c.page_size;
   const int64_t longest = std::max<int64_t>(1, std::min<int64_t>(b.max_kv_len, capacity));
   const int64_t rows = group * std::max(1, std::min(b.max_q_len, b.n_tokens));
-  const int64_t pairs = (int64_t)b.n_seq * c.kv_heads;
   L.many = rows > kFewRows;
   L.tiles = (int32_t)ceil_div(longest, many_keys(c.dim));
   // Parts of a 1024th of the batch's blocks of rows against tiles of keys, four
@@ -701,13 +713,21 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // are those that there are, however many requests have few of them.  One prompt of
   // 8192 over 16 heads on one KV head: 222 us, 274 with half as many parts, 439 with a
   // quarter; of 63 over 128 heads on 8, D = 64: 11.4 us, 15.3 with four blocks at
-  // least.  Up to 64 MB of sums.
-  const int64_t block = c.dim == 256 ? 32 : 64, keys = pairs * L.tiles * many_keys(c.dim) * 4;
-  const int64_t all = ceil_div((int64_t)b.n_tokens * group, block) * c.kv_heads * L.tiles;
-  const int64_t each = std::max<int64_t>(2, ceil_div(all, 1024));
-  const int64_t most = std::max<int64_t>(1, std::min(((int64_t)64 << 20) / keys, 65536 / (pairs * L.tiles)));
-  L.parts = (int32_t)std::min(ceil_div(rows, block * each), most);
-  if (L.many && L.parts > 1) L.bytes = keys * L.parts;
+  // least.  A prompt of 512 behind 1024 keys beside 31 single tokens, 32 heads on 8:
+  // 32 us, 73 with as many parts for each request as for the longest, most of them
+  // empty.  Up to 64 MB of sums.
+  const int64_t block = c.dim == 256 ? 32 : 64, all_rows = (int64_t)b.n_tokens * group;
+  const int64_t keys = (int64_t)c.kv_heads * L.tiles * many_keys(c.dim) * 4;  // sums of a part
+  int64_t each = std::max<int64_t>(2, ceil_div(ceil_div(all_rows, block) * c.kv_heads * L.tiles, 1024));
+  auto numbers = [&] { return ceil_div(all_rows, each * block) + b.n_seq; };
+  while (each * block < rows && numbers() * keys > (int64_t)64 << 20) each *= 2;
+  if (L.many && each * block < rows && numbers() * keys <= (int64_t)64 << 20) {
+    L.part_rows = (int32_t)(each * block);
+    L.numbers = (int32_t)numbers();
+    L.bytes = L.numbers * keys;
+  } else {
+    L.numbers = b.n_seq;
+  }
   return L;
 }
 
@@ -717,7 +737,7 @@ int weigh_launch(Args a, const Layout &L, int64_t longest, hipStream_t stream) {
   // Of few rows: 64 waves a CU, of 8 KB of keys at a time, if there are so many.
   const int64_t turns = ceil_div(longest, Few<TYPE, D>::keys);
   a.few_parts = (int32_t)std::min(turns, ceil_div(16384, pairs));
-  const int64_t few = pairs * a.few_parts, many = L.many ? pairs * L.tiles * L.parts : 0;
+  const int64_t few = pairs * a.few_parts, many = L.many ? (int64_t)L.numbers * a.kv_heads * L.tiles : 0;
   if (few * 64 + (many + 1) * 256 >= (int64_t)1 << 32 || few + many >= (int64_t)1 << 31)
     return ws_record_failure(WS_EUNSUPPORTED, "weigh: too many workgroups");
   if (!L.many) {
@@ -828,7 +848,8 @@ int wait_kv_weigh(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_k
     const int64_t longest = std::max<int64_t>(1, std::min<int64_t>(b.max_kv_len, capacity));
     a.both = L.many;
     a.tiles = L.tiles;
-    a.parts = L.parts;
+    a.part_rows = L.part_rows;
+    a.numbers = L.numbers;
     a.sums = (float *)d_workspace;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool bf = q->type == WS_KV_BF16;
