@@ -118,7 +118,8 @@ struct Few {
 };
 
 // Launches go round the 8 dies.  Four heads in a row go to one die, whose cache then
-// has the lines that the scales and weights of neighbouring heads share.
+// has the lines that the scales and weights of neighbouring heads share: 131 to 128 us
+// for the decode batch above.
 __device__ __forceinline__ int32_t near_pairs(int32_t id, int32_t pairs) {
   if (id >= pairs / 32 * 32) return id;
   return (id & ~31) | (id & 7) << 2 | (id >> 3 & 3);
@@ -275,7 +276,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a w
 // Of its 361 us in one run the products without the exponentials took 294, and all
 // but the copies 310: neither hides wholly behind the others.  32 keys a wave and
 // three workgroups a CU took 416 us, eight waves that share the copies 404.  The last
-// 32 of 131,072 tokens, 64 heads on 8, int8: 105 us, four blocks of rows for each 256
+// 32 of 131,072 tokens, 64 heads on 8, int8: 110 us, four blocks of rows for each 256
 // keys behind a start of several us; keeping the rows in shared memory from one tile
 // of keys to the next did not change that.
 
@@ -709,16 +710,20 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   L.many = rows > kFewRows;
   L.tiles = (int32_t)ceil_div(longest, many_keys(c.dim));
   // Parts of a 1024th of the batch's blocks of rows against tiles of keys, four
-  // workgroups a CU (causal, half of it is work), and of two blocks at least; the rows
-  // are those that there are, however many requests have few of them.  One prompt of
-  // 8192 over 16 heads on one KV head: 222 us, 274 with half as many parts, 439 with a
-  // quarter; of 63 over 128 heads on 8, D = 64: 11.4 us, 15.3 with four blocks at
-  // least.  A prompt of 512 behind 1024 keys beside 31 single tokens, 32 heads on 8:
-  // 32 us, 73 with as many parts for each request as for the longest, most of them
-  // empty.  Up to 64 MB of sums.
+  // workgroups a CU (causal, half of it is work); the rows are those that there are,
+  // however many requests have few of them.  One prompt of 8192 over 16 heads on one KV
+  // head: 222 us, 274 with half as many parts, 439 with a quarter.  A prompt of 512
+  // behind 1024 keys beside 31 single tokens, 32 heads on 8: 32 us, 73 with as many
+  // parts for each request as for the longest, most of them empty.
+  // A part has four blocks at least, where joining costs what it saves: the last 32 of
+  // 8192 tokens, 64 heads on 8, 17 us, 24 with two; two where there would be a
+  // workgroup for half of the CUs at most: 63 tokens, 128 heads on 8, D = 64, 11.4 us,
+  // 15.3 with four.  Up to 64 MB of sums.
   const int64_t block = c.dim == 256 ? 32 : 64, all_rows = (int64_t)b.n_tokens * group;
-  const int64_t keys = (int64_t)c.kv_heads * L.tiles * many_keys(c.dim) * 4;  // sums of a part
-  int64_t each = std::max<int64_t>(2, ceil_div(ceil_div(all_rows, block) * c.kv_heads * L.tiles, 1024));
+  const int64_t tiles = (int64_t)c.kv_heads * L.tiles;
+  const int64_t keys = tiles * many_keys(c.dim) * 4;  // sums of a part
+  const int64_t least = ceil_div(all_rows, rows) * tiles <= 128 ? 2 : 4;
+  int64_t each = std::max(least, ceil_div(ceil_div(all_rows, block) * tiles, 1024));
   auto numbers = [&] { return ceil_div(all_rows, each * block) + b.n_seq; };
   while (each * block < rows && numbers() * keys > (int64_t)64 << 20) each *= 2;
   if (L.many && each * block < rows && numbers() * keys <= (int64_t)64 << 20) {
