@@ -8,6 +8,7 @@ import torch
 
 from kv_more_util import kept_keys
 from paper_2504_11320_amd import binding as B
+from paper_2504_11320_amd import iteration as I
 from paper_2504_11320_amd import kv
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -289,3 +290,18 @@ def test_the_oracles_choice():
     assert kept_keys(w, 7, 0) == [0, 1, 2, 4, 5, 6, 7]
     assert kept_keys(w, 7, 7) == list(range(1, 8))
     assert kept_keys(w, 8, 3) == list(range(8)) and kept_keys(w[:0], 8, 3) == []
+
+
+def test_batches_on_a_budget():
+    """Stages hold at most the budget behind the iteration before; positions go on
+    where the tokens are, slots where the rows are."""
+    new, old = I.stage_batch(5, 3, 2, keep=6)
+    assert new == [5, 5, 1, 1, 1, 1, 1, 1] and old == [0, 0, 5, 5, 6, 6, 6, 6]
+    assert I.stage_batch(5, 3, 2) == I.stage_batch(5, 3, 2, keep=100)
+    b = I.Batch([1, 2], [6, 3], 4, device="cpu", at=[50, 3])
+    assert b.positions.tolist() == [50, 3, 4] and b.slots.tolist() == [6, 11, 12]
+    assert b.kv_lens.tolist() == [7, 5] and b.tokens == 12
+    for kw in (dict(keep=4, recent=5), dict(recent=1), dict(keep=-1), dict(keep=4, recent=-1)):
+        with pytest.raises(ValueError):
+            I.Shape(**kw)
+    assert I.Shape(keep=4, recent=4).keep == 4
