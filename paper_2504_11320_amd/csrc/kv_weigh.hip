@@ -143,7 +143,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a w
   if (k0 >= end) return;
 
   u32x4 q[F::steps];
-  float log[4];  // of rows 4 g + r
+  float log[4];  // of rows 4 g + r; -infinity: one that counts nothing, or none at all
   auto load_rows = [&](int32_t r0) {
     const int32_t row = r0 + n16;
     const bool live = row < rows;
@@ -165,7 +165,7 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a w
           q[i][j] = (uint32_t)p[d + 2 * j] | (uint32_t)p[d + 2 * j + 1] << 16;
       }
     }
-    const float l = live ? row_log(a.lse[at * a.heads + head]) : INFINITY;
+    const float l = live ? a.lse[at * a.heads + head] * kLog2E : -INFINITY;
 #pragma unroll
     for (int r = 0; r < 4; ++r) log[r] = __shfl(l, 4 * g + r);
   };
@@ -232,7 +232,11 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a w
         const float f = CODES ? __shfl(factor, 16 * t + n16) : factor;
         float p[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = exp2_of(__builtin_fmaf(z[t][r], f, -log[r]));
+        for (int r = 0; r < 4; ++r) {
+          // by a choice: a score that is not finite makes any sum with it NaN
+          p[r] = exp2_of(__builtin_fmaf(z[t][r], f, -log[r]));
+          p[r] = log[r] == -INFINITY ? 0.0f : p[r];
+        }
         if (!all) {
           const Range see = rows_of_key(a, s, k0 + 16 * t + n16, rows);
 #pragma unroll
