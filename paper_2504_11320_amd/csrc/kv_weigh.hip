@@ -74,7 +74,8 @@ __device__ __forceinline__ void codes_to_16(u32x4 x, u32x4 &lo, u32x4 &hi) {
   }
 }
 
-// log2(e) times a row's log-sum; one that saw nothing counts nothing.
+// log2(e) times a row's log-sum; one that saw nothing counts nothing of a score,
+// unless that is not finite, which leaves NaN.
 __device__ __forceinline__ float row_log(float lse) {
   return lse == -INFINITY ? INFINITY : lse * kLog2E;
 }
@@ -613,14 +614,52 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
     else
       finish(za);
     // the two halves' rows
-    float total = sum[0][0] + sum[0][1];
-    if constexpr (M::ktiles == 2) {
-      const float other = sum[1][0] + sum[1][1];
-      total = (hh ? other : total) + __shfl_xor(hh ? total : other, 32);
-    } else {
-      total += __shfl_xor(total, 32);
-    }
+    auto join = [&](const float (&x)[M::ktiles][2]) {
+      const float one = x[0][0] + x[0][1];
+      if constexpr (M::ktiles == 2) {
+        const float other = x[1][0] + x[1][1];
+        return (hh ? other : one) + __shfl_xor(hh ? one : other, 32);
+      } else {
+        return one + __shfl_xor(one, 32);
+      }
+    };
+    float total = join(sum);
     const bool has = key < end && lane < own;
+    if (__any(has && row_at != kNoRow && total != total)) {
+      // Again, rows that saw nothing left out by a choice, by the wave alone.  A choice
+      // in the loop above took 3 to 5 % more of everything.
+      float again[M::ktiles][2] = {};
+      for (int32_t r0 = max(some.lo, lo) / 32 * 32; r0 < some.hi; r0 += 32) {
+        const int32_t row = min(r0 + n32, rows - 1), token = row / a.group;
+        const int32_t head = h * a.group + row - token * a.group;
+        const int64_t at = s.q0 + token;
+        const char *q = (const char *)(a.q + at * a.qt + head * a.qh);
+        const float l = -a.lse[at * a.heads + head] * kLog2E;  // +infinity: saw nothing
+        f32x16 z[M::ktiles];
+#pragma unroll
+        for (int t = 0; t < M::ktiles; ++t) z[t] = f32x16{};
+#pragma unroll
+        for (int e = 0; e < M::steps; ++e) {
+          const int c = CODES ? 4 * (e / 2) + 2 * hh + e % 2 : 2 * e + hh;
+          product(z, *reinterpret_cast<const u32x4 *>(q + 16 * c), e);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int32_t in = 8 * (r / 4) + 4 * hh + r % 4;
+          const float log = __shfl(l, in);
+#pragma unroll
+          for (int t = 0; t < M::ktiles; ++t) {
+            const Range see = rows_of_key(a, s, k0 + 32 * t + n32, rows);
+            const float p = exp2_of(__builtin_fmaf(z[t][r], f[t], log));
+            const bool counts =
+                (r0 + in >= see.lo) & (r0 + in < min(see.hi, hi)) & (log != INFINITY);
+            again[t][r & 1] += counts ? p : 0.0f;
+          }
+        }
+      }
+      const float chosen = join(again);
+      total = total != total ? chosen : total;
+    }
     if (split.parts > 1) {
       const int64_t number = first_part(a, b) + part;  // again: registers are short above
       if (has) a.sums[(number * a.kv_heads + h) * a.tiles * M::keys + key] = total;

@@ -60,3 +60,52 @@ def test_an_infinite_scale_that_nobody_attends_to(dtype, heads):
         old = j < kl[b] - ql[b]
         want[at], tol[at] = float(w[at]) if old else 0.0, 0.0
     within(weigh(q, lse, c, pages, starts, lens, w), want, tol, "beside an infinite scale")
+
+
+def idle_rows(ql, kl, heads, dim, dtype, cache_dtype, seed, **kw):
+    """Rows under a log-sum of -infinity, among them all of a request's last
+    token and of a whole request: whatever their queries hold, and the keys that
+    only they see, they count nothing."""
+    q, pages, starts, lens, n = batch(ql, kl, 16, heads, dim, dtype, seed)
+    c = fill(n, 16, 1, dim, cache_dtype, seed + 1)
+    lse = attend(q, c, pages, starts, lens, **kw)[1].float()
+    g = torch.Generator().manual_seed(seed + 2)
+    idle = torch.rand(lse.shape, generator=g) < 0.1
+    for b in range(len(ql)):
+        idle[int(starts[b + 1]) - 1] = True
+    idle[int(starts[-2]):] = True
+    lse[idle] = -math.inf
+    w = torch.rand(n, 1, 16, generator=g)
+    want, tol = weighed(q, lse, c, pages, starts, lens, w, **kw)
+    # what must not count: queries that are not finite, and where causal each
+    # request's last key, which its last token alone sees
+    bad = torch.tensor([math.nan, math.inf, -math.inf])
+    at = idle.nonzero()
+    q[at[:, 0], at[:, 1], torch.arange(len(at)) % dim] = bad[torch.arange(len(at)) % 3].to(dtype)
+    if kw.get("causal", True):
+        for b, m in enumerate(kl):
+            row = int(pages[b, (m - 1) // 16]), 0, (m - 1) % 16
+            if c.k_scale is None:
+                c.k[row] = float(bad[b % 3])
+            else:
+                c.k_scale[row] = float(bad[b % 3])
+    got = weigh(q, lse, c, pages, starts, lens, w, **kw)
+    within(got, want, tol, f"idle rows of {ql}")
+
+
+@pytest.mark.parametrize("cache_dtype", [torch.bfloat16, torch.float16, torch.float8_e4m3fn,
+                                         torch.int8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads", [1, 7, 16])
+def test_rows_that_saw_nothing_count_nothing(cache_dtype, dim, heads):
+    dtype = cache_dtype if cache_dtype.itemsize == 2 else torch.float16
+    idle_rows([1, 3, 1, 2], [70, 50, 16, 33], heads, dim, dtype, cache_dtype, 41)
+    idle_rows([1, 150, 3, 40], [70, 200, 16, 133], heads, dim, dtype, cache_dtype, 51)
+    idle_rows([150, 40], [200, 133], heads, dim, dtype, cache_dtype, 61, causal=False)
+    idle_rows([150, 40], [200, 133], heads, dim, dtype, cache_dtype, 71, window=60)
+
+
+def test_rows_that_saw_nothing_in_parts():
+    """Rows split over workgroups, more blocks of rows than one turn of the ring."""
+    idle_rows([900, 70], [900, 90], 4, 128, torch.bfloat16, torch.bfloat16, 81)
+    idle_rows([500, 70], [900, 90], 16, 64, torch.float16, torch.int8, 91, causal=False)
