@@ -32,8 +32,9 @@ int wait_kv_weigh_workspace_bytes(const ws_kv_cache *cache, const ws_kv_batch *b
  * and j < kv_len - n: the batch's own n tokens are new, and start from zero
  * whatever their rows held.  Rows whose log-sum is -infinity saw nothing and
  * count nothing.  Keys that are not there (wait_kv.h) have no weight.  Two
- * requests must not share pages.  Sums are taken in a fixed order: the same call
- * gives the same bits.  The workspace holds nothing between calls; calls that
+ * requests must not share pages, nor the weights memory with the cache or another
+ * input.  Sums are taken in a fixed order: the same call gives the same bits.  The
+ * workspace is memory of its own, and holds nothing between calls; calls that
  * overlap need one each. */
 int wait_kv_weigh(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_kv_rows *q,
                   const float *lse, float *weights, int32_t accumulate, void *d_workspace,

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 #include <new>
 
 #include "wait_kv.h"
@@ -58,6 +59,48 @@ inline int check_rows(const ws_kv_rows *r, int64_t n, const char *null_msg) {
   return WS_OK;
 }
 
+// Memory from lo to hi - 1, and whether two share some.
+struct Span {
+  __int128 lo, hi;
+};
+inline Span span(const void *p, __int128 bytes) {
+  const __int128 lo = (uintptr_t)p;
+  return {lo, p && bytes > 0 ? lo + bytes : lo};
+}
+// From the first to the last element of a batch's vectors.
+inline Span span(const ws_kv_rows &r, int64_t n, int64_t heads, int64_t dim) {
+  using wide = __int128;
+  if (n < 1 || heads < 1 || dim < 1) return span(nullptr, 0);
+  const wide e = type_bytes(r.type), none = 0;
+  const wide tokens = (wide)(n - 1) * r.token_stride * e, step = (wide)(heads - 1) * r.head_stride * e;
+  const wide at = (wide)(uintptr_t)r.data;
+  return {at + (tokens < none ? tokens : none) + (step < none ? step : none),
+          at + (tokens > none ? tokens : none) + (step > none ? step : none) + dim * e};
+}
+inline bool shares(const Span &a, const Span &b) {
+  return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
+}
+inline bool shares(const Span &a, std::initializer_list<Span> others) {
+  for (const Span &b : others)
+    if (shares(a, b)) return true;
+  return false;
+}
+// A cache's memory, and that of a batch's page table.
+struct CacheSpans {
+  Span k, v, ks, vs;
+  explicit CacheSpans(const ws_kv_cache &c) {
+    const __int128 rows = (__int128)c.pages * c.kv_heads * c.page_size;
+    k = span(c.k, rows * c.dim * type_bytes(c.type));
+    v = span(c.v, rows * c.dim * type_bytes(c.type));
+    ks = span(c.k_scale, rows * 4);
+    vs = span(c.v_scale, rows * 4);
+  }
+};
+inline bool shares(const Span &a, const CacheSpans &c) { return shares(a, {c.k, c.v, c.ks, c.vs}); }
+inline Span table_span(const int32_t *table, int64_t n_seq, int64_t stride, int64_t cols) {
+  return span(table, n_seq > 0 ? 4 * ((__int128)(n_seq - 1) * stride + cols) : 0);
+}
+
 // Whether vectors of a share memory with vectors of b: n tokens of heads_a and
 // heads_b of dim elements of one size each.  Exact where the token strides are the
 // same, as of parts of one buffer's rows; others share it if their ranges meet.
@@ -66,22 +109,12 @@ inline bool overlap(const ws_kv_rows &a, const ws_kv_rows &b, int64_t n, int64_t
   using wide = __int128;
   if (n < 1 || heads_a < 1 || heads_b < 1 || dim < 1) return false;
   const wide e = type_bytes(a.type), len = dim * e;
-  struct Span {
-    wide at, lo, hi;
-  };
-  auto span = [&](const ws_kv_rows &r, int64_t heads) {
-    const wide tokens = (wide)(n - 1) * r.token_stride * e, step = (wide)(heads - 1) * r.head_stride * e;
-    const wide at = (wide)(uintptr_t)r.data, none = 0;
-    return Span{at, at + (tokens < 0 ? tokens : none) + (step < 0 ? step : none),
-                at + (tokens > 0 ? tokens : none) + (step > 0 ? step : none) + len};
-  };
-  const Span x = span(a, heads_a), y = span(b, heads_b);
-  if (x.hi <= y.lo || y.hi <= x.lo) return false;
+  if (!shares(span(a, n, heads_a, dim), span(b, n, heads_b, dim))) return false;
   if (n > 1 && a.token_stride != b.token_stride) return true;
   // heads i of a and j of b are `apart` bytes apart at one token, and by a
   // multiple of `step` more at others
   const wide step = n > 1 ? (wide)a.token_stride * e : 0;
-  auto meet = [&](wide apart) {
+  auto near = [&](wide apart) {
     wide k = step ? -apart / step : 0;  // towards zero: k or a neighbour is nearest
     for (wide d = k - 1; d <= k + 1; ++d) {
       if (d <= -n || d >= n) continue;
@@ -94,7 +127,8 @@ inline bool overlap(const ws_kv_rows &a, const ws_kv_rows &b, int64_t n, int64_t
   for (int64_t i = 0; i < heads_a; ++i)
     for (int64_t j = 0; j < heads_b; ++j) {
       if (same && i && j) break;  // differences of heads, each once
-      if (meet(y.at - x.at + ((wide)j * b.head_stride - (wide)i * a.head_stride) * e)) return true;
+      const wide apart = (wide)(uintptr_t)b.data - (wide)(uintptr_t)a.data;
+      if (near(apart + ((wide)j * b.head_stride - (wide)i * a.head_stride) * e)) return true;
     }
   return false;
 }

@@ -810,12 +810,6 @@ int weigh_dim(int dim, const Args &a, const Layout &L, int64_t longest, hipStrea
   return weigh_launch<TYPE, BF, 256>(a, L, longest, stream);
 }
 
-// Whether byte ranges meet.
-bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
-  const char *x = (const char *)a, *y = (const char *)b;
-  return na > 0 && nb > 0 && x < y + nb && y < x + na;
-}
-
 }  // namespace
 
 extern "C" {
@@ -849,17 +843,24 @@ int wait_kv_weigh(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_k
       return invalid("weigh: the page table, starts and lengths must be non-NULL");
     if ((uintptr_t)b.starts % 4 || (uintptr_t)b.kv_lens % 4 || (uintptr_t)b.table % 4)
       return invalid("weigh: the page table, starts and lengths must be aligned to 4 bytes");
-    const int64_t cells = (int64_t)cache->pages * cache->kv_heads * cache->page_size;
-    if (overlap(weights, cells * 4, lse, (int64_t)b.n_tokens * b.heads * 4) ||
-        overlap(weights, cells * 4, cache->k, cells * cache->dim * type_bytes(cache->type)) ||
-        (cache->k_scale && overlap(weights, cells * 4, cache->k_scale, cells * 4)))
-      return invalid("weigh: the weights must not overlap the log-sums or the keys");
+    const Span w = span(weights, (__int128)cache->pages * cache->kv_heads * cache->page_size * 4);
+    const CacheSpans in_cache(*cache);
+    auto taken = [&](const Span &x) {  // by what the call reads
+      return shares(x, in_cache) ||
+             shares(x, {span(*q, b.n_tokens, b.heads, cache->dim),
+                      span(lse, (__int128)b.n_tokens * b.heads * 4),
+                      table_span(b.table, b.n_seq, b.table_stride, b.table_cols),
+                      span(b.starts, 4 * ((__int128)b.n_seq + 1)), span(b.kv_lens, 4 * (__int128)b.n_seq)});
+    };
+    if (taken(w)) return invalid("weigh: the weights must not overlap the cache, q or another input");
     const int64_t capacity = (int64_t)b.table_cols * cache->page_size;
     if (capacity == 0) return WS_OK;
     Layout L = layout_of(*cache, b);
     if (L.bytes && (!d_workspace || ws_bytes < (size_t)L.bytes))
       return ws_record_failure(WS_EWORKSPACE, "weigh: the workspace is too small");
     if ((uintptr_t)d_workspace % 4) return invalid("weigh: the workspace must be aligned to 4 bytes");
+    const Span space = span(d_workspace, L.bytes);
+    if (shares(space, w) || taken(space)) return invalid("weigh: the workspace must be its own memory");
     // many rows are copied 16 bytes at a time, a block's from one address with
     // offsets of 32 bits
     const int64_t group = b.heads / cache->kv_heads, block = 64 / group + 2;

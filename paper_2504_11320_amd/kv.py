@@ -310,7 +310,8 @@ def weigh(q: torch.Tensor, lse: torch.Tensor, cache: Cache, pages: torch.Tensor,
     request b, are new and start from zero, whatever their rows held; without
     ``accumulate`` all keys of the batch's requests do (so that the last tokens of
     a prompt alone can say which of its keys matter).  Keys of other requests stay
-    as they are.  Requests must not share pages.  ``workspace`` (a uint8 tensor of
+    as they are.  Requests must not share pages, nor ``weights`` memory with the
+    cache or another argument.  ``workspace`` (a uint8 tensor of
     ``weigh_workspace_bytes``) is taken from PyTorch where it is not given."""
     _native().weigh(cache._c, cache._index, q, pages, starts, kv_lens, max_q_len, max_kv_len, scale,
                     causal, window, lse, weights, accumulate, workspace)

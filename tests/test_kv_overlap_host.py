@@ -1,0 +1,49 @@
+"""Memory that a call would write over while it reads it, or that is not its to
+write, is refused: the C ABI, on addresses that are never dereferenced."""
+import pytest
+
+from paper_2504_11320_amd import binding as B
+from paper_2504_11320_amd import kv
+from test_kv_more_host import batch, cache, rows
+
+AT = 1 << 44   # memory of every argument, far from the others'
+K, V, KS, VS, Q, OUT, LSE, W, TABLE, LENS, KEPT, LEFT, WS, TO, SLOTS = (AT + (i << 32) for i in range(15))
+
+
+def eight(**kw):
+    return cache(**{**dict(k=K, v=V, k_scale=KS, v_scale=VS, type=kv.INT8), **kw})
+
+
+def sixteen(**kw):
+    return cache(**{**dict(k=K, v=V), **kw})
+
+
+def refused(rc, what="overlap"):
+    assert rc == B.WS_EINVAL
+    assert what in kv._lib().wait_sim_last_error().decode()
+
+
+# a cache of 4 pages of 16 rows of 2 heads of 64: 128 rows
+ROWS, ROW8, ROW16 = 128, 64, 128
+
+
+def weigh(c, w=W, ws=None, bytes_=0, **kw):
+    b = dict(table=TABLE, starts=LENS + 4096, kv_lens=LENS)
+    return kv._lib().wait_kv_weigh(c, batch(**{**b, **kw}), rows(data=Q, token=256), LSE, w, 1, ws, bytes_,
+                                   None)
+
+
+@pytest.mark.parametrize("w", [K, K + ROWS * ROW8 - 4, V, V + ROWS * ROW8 - 4, KS, VS, VS + 4 * ROWS - 4,
+                               VS - 4 * ROWS + 4, Q, Q + 3 * 512 + 4 * 128 - 4, LSE, LSE + 4 * 4 * 4 - 4, TABLE,
+                               TABLE + 4 * 15, LENS, LENS + 4, LENS + 4096])
+def test_weights_that_lie_in_something_else(w):
+    refused(weigh(eight(), w=w))
+    if not KS - 4096 <= w < VS + 4096:
+        refused(weigh(sixteen(), w=w))
+
+
+def test_a_workspace_that_lies_in_something_else():
+    many = dict(n_tokens=512, max_q_len=512, max_kv_len=128)
+    assert weigh(eight(), **many) == B.WS_EWORKSPACE
+    for ws in (K, V, KS, VS, Q, LSE, W, W + 4 * ROWS - 4, TABLE, LENS):
+        refused(weigh(eight(), ws=ws, bytes_=1 << 26, **many), "workspace")
