@@ -74,8 +74,10 @@ int wait_kv_evict_workspace_bytes(const ws_kv_cache *cache, const ws_kv_eviction
                                   size_t *bytes);
 
 /* kept [n_seq][kv_heads][keep] int32: the kept keys' indices, -1 behind them;
- * new_lens [n_seq]: min(kv_lens, keep), in memory of its own.  The workspace holds
- * nothing between calls; calls that overlap need one each. */
+ * new_lens [n_seq]: min(kv_lens, keep).  Weights, outputs and workspace have memory
+ * of their own, apart from one another, the cache, its page tables and the lengths;
+ * so have keys and values that move in place.  The workspace holds nothing between
+ * calls; calls that overlap need one each. */
 int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, float *weights,
                   int32_t *kept, int32_t *new_lens, void *d_workspace, size_t ws_bytes,
                   void *hip_stream);

@@ -654,6 +654,23 @@ int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, floa
     if (bytes && (!d_workspace || ws_bytes < (size_t)bytes))
       return ws_record_failure(WS_EWORKSPACE, "evict: the workspace is too small");
     if ((uintptr_t)d_workspace % 16) return invalid("evict: the workspace must be 16-byte aligned");
+    const CacheSpans in_cache(*cache);
+    const Span w = span(weights, (__int128)cache->pages * cache->kv_heads * cache->page_size * 4);
+    const Span list = span(kept, (__int128)pairs * e.keep * 4), lens = span(new_lens, (__int128)e.n_seq * 4);
+    const Span space = span(d_workspace, bytes);
+    const Span read[3] = {table_span(e.table, e.n_seq, e.table_stride, e.table_cols),
+                          table_span(e.to, e.n_seq, e.to_stride, e.to_cols),
+                          span(e.kv_lens, (__int128)e.n_seq * 4)};
+    for (const Span &in : read)
+      if (shares(in, in_cache) || shares(in, {w, list, lens}))
+        return invalid("evict: weights, outputs and cache must not overlap the lengths or the pages");
+    if (shares(w, in_cache) || shares(list, in_cache) || shares(lens, in_cache) || shares(w, {list, lens}) ||
+        shares(list, lens))
+      return invalid("evict: weights and outputs must not overlap the cache or one another");
+    if (shares(space, in_cache) || shares(space, {w, list, lens, read[0], read[1], read[2]}))
+      return invalid("evict: the workspace must be its own memory");
+    if (!e.to && (shares(in_cache.k, in_cache.v) || shares(in_cache.ks, in_cache.vs)))
+      return invalid("evict: keys and values that move in place must not overlap");
     Args a{};
     a.k = (char *)cache->k;
     a.v = (char *)cache->v;

@@ -4,7 +4,7 @@ import pytest
 
 from paper_2504_11320_amd import binding as B
 from paper_2504_11320_amd import kv
-from test_kv_more_host import batch, cache, rows
+from test_kv_more_host import batch, cache, eviction, rows
 
 AT = 1 << 44   # memory of every argument, far from the others'
 K, V, KS, VS, Q, OUT, LSE, W, TABLE, LENS, KEPT, LEFT, WS, TO, SLOTS = (AT + (i << 32) for i in range(15))
@@ -23,7 +23,7 @@ def refused(rc, what="overlap"):
     assert what in kv._lib().wait_sim_last_error().decode()
 
 
-# a cache of 4 pages of 16 rows of 2 heads of 64: 128 rows
+# a cache of 4 pages of 16 rows of 2 heads of 64: 128 rows, 16-bit ones of 128 bytes
 ROWS, ROW8, ROW16 = 128, 64, 128
 
 
@@ -43,7 +43,42 @@ def test_weights_that_lie_in_something_else(w):
 
 
 def test_a_workspace_that_lies_in_something_else():
+    """Weighing: rows that are split need one."""
     many = dict(n_tokens=512, max_q_len=512, max_kv_len=128)
     assert weigh(eight(), **many) == B.WS_EWORKSPACE
     for ws in (K, V, KS, VS, Q, LSE, W, W + 4 * ROWS - 4, TABLE, LENS):
         refused(weigh(eight(), ws=ws, bytes_=1 << 26, **many), "workspace")
+    long = dict(table_cols=1 << 10, table_stride=1 << 10, max_kv_len=10000)
+    assert evict(eight(), **long) == B.WS_EWORKSPACE
+    for ws in (K, V, KS, VS, W, TABLE, LENS, KEPT, LEFT):
+        refused(evict(eight(), ws=ws, bytes_=1 << 26, **long), "workspace")
+
+
+def evict(c, w=W, kept=KEPT, left=LEFT, ws=None, bytes_=0, **kw):
+    e = dict(table=TABLE, kv_lens=LENS)
+    return kv._lib().wait_kv_evict(c, eviction(**{**e, **kw}), w, kept, left, ws, bytes_, None)
+
+
+@pytest.mark.parametrize("to", [0, TO])
+def test_an_eviction_into_its_own_arguments(to):
+    kw = dict(to=to)
+    for w in (K, V, KS, VS, VS + 4 * ROWS - 4, TABLE, LENS):
+        refused(evict(eight(), w=w, **kw))
+    for at in (K, V + ROWS * ROW8 - 4, KS, VS, W, W + 4 * ROWS - 4, TABLE, LENS):
+        refused(evict(eight(), kept=at, **kw))
+        if at != LENS:
+            refused(evict(eight(), left=at, **kw))
+    refused(evict(eight(), left=LENS + 4, **kw), "memory of their own")
+    refused(evict(eight(), left=KEPT + 4 * 2 * 2 * 20 - 4, **kw))
+    refused(evict(eight(k=TABLE), **kw))
+    refused(evict(sixteen(v=LENS), **kw))
+    if to:
+        refused(evict(eight(), w=TO, **kw))
+        refused(evict(eight(), kept=TO + 4 * 3, **kw))
+
+
+def test_keys_and_values_of_one_place():
+    """Rows that move within their pages go there once."""
+    refused(evict(sixteen(v=K)))
+    refused(evict(sixteen(v=K + ROWS * ROW16 - 16)))
+    refused(evict(eight(v_scale=KS)))
