@@ -42,7 +42,7 @@ int wait_kv_norm_rotary(const ws_kv_rows *x, const ws_kv_rows *out, int64_t n, i
  * v [n][kv_heads] of the cache into slots[i], as wait_kv_append puts them there,
  * k by k_norm and turn.  One turn for both; either norm and the turn may be
  * NULL.  q, q_out, k and v have one type.  q_out may be q itself and shares no
- * memory with k or v.  A row whose slot is outside the cache gives its queries
+ * memory with k, v or the cache.  A row whose slot is outside the cache gives its queries
  * all the same. */
 int wait_kv_enter(const ws_kv_cache *cache, const ws_kv_rows *q, const ws_kv_rows *q_out,
                   int32_t heads, const ws_kv_rows *k, const ws_kv_rows *v, const int64_t *slots,

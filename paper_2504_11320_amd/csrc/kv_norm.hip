@@ -590,6 +590,8 @@ int wait_kv_enter(const ws_kv_cache *cache, const ws_kv_rows *q, const ws_kv_row
     for (const ws_kv_rows *r : {k, v})
       if (overlap(*q_out, *r, n, heads, cache->kv_heads, cache->dim))
         return invalid("enter: q's output must not overlap k or v");
+    if (shares(span(*q_out, n, heads, cache->dim), CacheSpans(*cache)))
+      return invalid("enter: q's output must not overlap the cache");
     if (n == 0) return WS_OK;
     Args a{};
     a.q = side(*q, q_norm);

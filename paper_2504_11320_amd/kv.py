@@ -239,7 +239,7 @@ def enter(cache: Cache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots
     it a side is not normed, without ``positions`` and ``table`` neither is
     turned.  A token without a slot gives its queries all the same.  ``out`` may
     be q, which may lie beside k and v in the rows of one product, and must not
-    overlap q otherwise, nor k or v."""
+    overlap q otherwise, nor k, v or the cache."""
     return _native().enter(cache._c, cache._index, cache._tensors, q, k, v, slots, positions, table,
                            q_norm, k_norm, eps, interleaved, out)
 

@@ -4,7 +4,7 @@ import pytest
 
 from paper_2504_11320_amd import binding as B
 from paper_2504_11320_amd import kv
-from test_kv_more_host import batch, cache, eviction, rows
+from test_kv_more_host import batch, cache, eviction, norm, rows, turn
 
 AT = 1 << 44   # memory of every argument, far from the others'
 K, V, KS, VS, Q, OUT, LSE, W, TABLE, LENS, KEPT, LEFT, WS, TO, SLOTS = (AT + (i << 32) for i in range(15))
@@ -82,3 +82,17 @@ def test_keys_and_values_of_one_place():
     refused(evict(sixteen(v=K)))
     refused(evict(sixteen(v=K + ROWS * ROW16 - 16)))
     refused(evict(eight(v_scale=KS)))
+
+
+def test_queries_that_enter_the_cache():
+    q, k, v = (rows(data=Q + 128 * i, token=512) for i in (0, 4, 6))
+
+    def enter(out, c):
+        return kv._lib().wait_kv_enter(c, q, rows(data=out, token=256), 4, k, v, SLOTS, 3, norm(), norm(), turn(),
+                                       None)
+
+    for c, row in ((eight(), ROW8), (sixteen(), ROW16)):
+        for at in (K, K + ROWS * row - 2, K - 3 * 512 + 2, V, V + ROWS * row - 2):
+            refused(enter(at, c))
+    for at in (KS, VS, VS + 4 * ROWS - 2):
+        refused(enter(at, eight()))
