@@ -69,7 +69,8 @@ typedef struct {
   int32_t max_kv_len;
 } ws_kv_eviction;
 
-/* Bytes of workspace that wait_kv_evict takes (0 where requests are short). */
+/* Bytes of workspace that wait_kv_evict takes: 0 where requests are short, at most
+ * 256 MB. */
 int wait_kv_evict_workspace_bytes(const ws_kv_cache *cache, const ws_kv_eviction *eviction,
                                   size_t *bytes);
 

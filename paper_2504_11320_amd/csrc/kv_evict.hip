@@ -38,7 +38,7 @@ struct Args {
   int32_t parts;     // of a request's keys, that are counted
   int32_t *counts;   // [digit][request][KV head][part][256]
   Found *found;      // [request][KV head][part]
-  uint32_t *orders;  // [request][KV head][part][kPart]: the weights as whole numbers
+  uint32_t *orders;  // [request][KV head][part][kPart]: the weights as whole numbers; or NULL
 };
 
 __device__ __forceinline__ int32_t length_of(const Args &a, int32_t b) {
@@ -355,10 +355,11 @@ __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
   __shared__ Shared sh;
   const int32_t part = blockIdx.x % a.parts, pair = blockIdx.x / a.parts;
   // asked for before anything is known; the first launch leaves the numbers where
-  // they need no page table
-  uint32_t *left_here = a.orders + (int64_t)blockIdx.x * kPart;
+  // they need no page table, if there is room
+  const bool room = a.orders != nullptr;
+  uint32_t *left_here = a.orders + (room ? (int64_t)blockIdx.x * kPart : 0);
   Held<16> k;
-  if (digit > 0) k.load_left(left_here);
+  if (digit > 0 && room) k.load_left(left_here);
   const Pair p(a, pair);
   int32_t *kept = a.kept + (int64_t)pair * a.keep;
   if (digit == 4 && p.h == 0 && part == 0 && threadIdx.x == 0)
@@ -371,9 +372,10 @@ __global__ void __launch_bounds__(256) count_kernel(Args a, int digit) {
   }
   const Range r = part_of(a, part, p.n);
   auto order = [&](int32_t j) { return p.order(a, j); };
-  if (r.lo < r.hi && (digit == 0 || r.hi - r.lo > kPart)) {
+  const bool whole = room && r.hi - r.lo <= kPart;  // the numbers of all of its keys
+  if (r.lo < r.hi && (digit == 0 || !whole)) {
     k.load(r.lo, min(r.hi, r.lo + kPart), order);
-    if (digit == 0 && r.hi - r.lo <= kPart) k.leave(left_here);
+    if (digit == 0 && whole) k.leave(left_here);
   }
   Found f = {0, p.need, 0, 0};
   int32_t equal = 0;
@@ -560,15 +562,30 @@ __global__ void __launch_bounds__(256) close_up_kernel(Args a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The parts that a request's keys are counted in; 0 where they are not, or where the
-// last ones alone stay.
-int32_t parts_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
+// How the keys are counted.
+struct Layout {
+  int32_t parts;  // of a request's keys; 0 where they are not counted
+  bool orders;    // their numbers are kept
+  int64_t bytes;
+};
+constexpr int64_t kMost = (int64_t)256 << 20;  // bytes of workspace
+
+// A part has 4096 keys, unless their counts would take more than 256 MB: then there
+// are fewer and longer ones, or a workgroup alone finds a request's and head's keys.
+// The numbers are kept where they fit beside the counts: 64 requests of 32,768 keys,
+// 32 heads of 64 fp8, 1028 us with them (336 MB), 1090 without; 128 of 131,072, 8
+// heads, 1196 (840 MB) and 1378.
+Layout layout_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
+  Layout L{};
   const int64_t longest = std::min<int64_t>(e.max_kv_len, (int64_t)e.table_cols * c.page_size);
-  return longest <= kHeld || e.keep == e.recent ? 0 : (int32_t)ceil_div(longest, kPart);
-}
-int64_t bytes_of(const ws_kv_cache &c, const ws_kv_eviction &e) {
-  return (int64_t)e.n_seq * c.kv_heads * parts_of(c, e) *
-         (4 * 256 * 4 + (int64_t)sizeof(Found) + kPart * 4);
+  const int64_t pairs = (int64_t)e.n_seq * c.kv_heads;
+  if (longest <= kHeld || e.keep == e.recent || pairs == 0) return L;
+  const int64_t counts = pairs * (4 * 256 * 4 + (int64_t)sizeof(Found)), orders = pairs * kPart * 4;
+  const int64_t parts = ceil_div(longest, kPart);
+  L.orders = parts <= kMost / (counts + orders);
+  L.parts = (int32_t)std::min(parts, kMost / counts);
+  L.bytes = L.parts * (counts + (L.orders ? orders : 0));
+  return L;
 }
 
 int check_eviction(const ws_kv_cache *c, const ws_kv_eviction *e) {
@@ -630,7 +647,7 @@ int wait_kv_evict_workspace_bytes(const ws_kv_cache *cache, const ws_kv_eviction
   return guarded([&]() -> int {
     if (!bytes) return invalid("bytes must be non-NULL");
     if (int rc = check_eviction(cache, eviction)) return rc;
-    *bytes = (size_t)bytes_of(*cache, *eviction);
+    *bytes = (size_t)layout_of(*cache, *eviction).bytes;
     return WS_OK;
   });
 }
@@ -650,7 +667,8 @@ int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, floa
     const int64_t pairs = (int64_t)e.n_seq * cache->kv_heads;
     if (e.kv_lens < new_lens + e.n_seq && new_lens < e.kv_lens + e.n_seq)
       return invalid("evict: the new lengths need memory of their own");
-    const int64_t bytes = bytes_of(*cache, e);
+    const Layout L = layout_of(*cache, e);
+    const int64_t bytes = L.bytes;
     if (bytes && (!d_workspace || ws_bytes < (size_t)bytes))
       return ws_record_failure(WS_EWORKSPACE, "evict: the workspace is too small");
     if ((uintptr_t)d_workspace % 16) return invalid("evict: the workspace must be 16-byte aligned");
@@ -690,12 +708,12 @@ int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, floa
     a.page_shift = log2_of(cache->page_size);
     a.keep = e.keep;
     a.recent = e.recent;
-    a.parts = parts_of(*cache, e);
+    a.parts = L.parts;
     a.blocks = 1;
     if (bytes) {
       a.found = (Found *)d_workspace;
       a.counts = (int32_t *)(a.found + pairs * a.parts);
-      a.orders = (uint32_t *)(a.counts + pairs * a.parts * 4 * 256);
+      if (L.orders) a.orders = (uint32_t *)(a.counts + pairs * a.parts * 4 * 256);
     }
     hipStream_t s = (hipStream_t)hip_stream;
     switch (cache->dim * type_bytes(cache->type) / 16) {

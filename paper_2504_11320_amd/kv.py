@@ -352,6 +352,6 @@ def evict(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, weights: tor
 def evict_workspace_bytes(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, *, keep: int,
                           recent: int = 0, to: Optional[torch.Tensor] = None,
                           max_kv_len: Optional[int] = None) -> int:
-    """Bytes that ``evict`` takes as its workspace for these shapes."""
+    """Bytes that ``evict`` takes as its workspace for these shapes, up to 256 MB."""
     return _native().evict_workspace_bytes(cache._c, cache._index, pages, kv_lens, keep, recent, to,
                                            max_kv_len)
