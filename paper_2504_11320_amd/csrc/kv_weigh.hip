@@ -118,22 +118,23 @@ struct Few {
   static constexpr int keys = 16 * tiles;
 };
 
-// Launches go round the 8 dies.  Four heads in a row go to one die, whose cache then
-// has the lines that the scales and weights of neighbouring heads share: 131 to 128 us
-// for the decode batch above.
+// Launches go round the 8 dies.  Of waves that are workgroups, those of four heads in
+// a row go to one die, whose cache then has the lines that the scales and weights of
+// neighbouring heads share: 131 to 128 us for the decode batch above.  (Four waves of
+// one workgroup have neighbouring heads as they are numbered.)
 __device__ __forceinline__ int32_t near_pairs(int32_t id, int32_t pairs) {
   if (id >= pairs / 32 * 32) return id;
   return (id & ~31) | (id & 7) << 2 | (id >> 3 & 3);
 }
 
-template <int TYPE, bool BF, int D>
+template <int TYPE, bool BF, int D, bool ALONE>
 __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a wave
   using F = Few<TYPE, D>;
   constexpr bool CODES = kCodes<TYPE>;
   const int lane = threadIdx.x & 63;
   const int n16 = lane & 15, g = lane >> 4, mine = lane & (F::keys - 1);
   const int32_t pairs = a.n_seq * a.kv_heads;
-  const int32_t part = id / pairs, pair = near_pairs(id % pairs, pairs);
+  const int32_t part = id / pairs, pair = ALONE ? near_pairs(id % pairs, pairs) : id % pairs;
   if (part >= a.few_parts) return;
   const int32_t h = pair % a.kv_heads, b = pair / a.kv_heads;
   const Seq s = get_seq(a, b);
@@ -671,7 +672,7 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
 
 template <int TYPE, bool BF, int D>
 __global__ void __launch_bounds__(64, 2) few_kernel(Args a) {
-  few_rows<TYPE, BF, D>(a, blockIdx.x);
+  few_rows<TYPE, BF, D, true>(a, blockIdx.x);
 }
 
 template <int TYPE, bool BF, int D>
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(256, 2) many_kernel(Args a, int32_t many) {
   if ((int32_t)blockIdx.x < many)
     many_rows<TYPE, BF, D>(a, blockIdx.x, smem);
   else
-    few_rows<TYPE, BF, D>(
+    few_rows<TYPE, BF, D, false>(
         a, __builtin_amdgcn_readfirstlane((blockIdx.x - many) * 4 + (threadIdx.x >> 6)));
 }
 
