@@ -61,8 +61,10 @@ class Shape:
         return self.heads * self.dim
 
     def token_bytes(self) -> int:
-        """KV cache bytes of a token, all layers."""
-        return self.layers * kv.Cache.token_bytes(self.kv_heads, self.dim, self.cache)
+        """KV cache bytes of a token, all layers; with ``keep`` also what its keys
+        have received."""
+        return self.layers * (kv.Cache.token_bytes(self.kv_heads, self.dim, self.cache)
+                              + (4 * self.kv_heads if self.keep else 0))
 
 
 def budget(shape: Shape, nbytes: float) -> int:
