@@ -597,6 +597,8 @@ int check_eviction(const ws_kv_cache *c, const ws_kv_eviction *e) {
   if (e->max_kv_len < 0) return invalid("evict: bad length bound");
   if ((int64_t)e->table_cols * c->page_size >= (int64_t)1 << 30 || e->keep >= 1 << 30)
     return ws_record_failure(WS_EUNSUPPORTED, "evict: 2^30 keys a request or more");
+  if ((int64_t)e->n_seq * c->kv_heads >= (int64_t)1 << 24)  // a workgroup each
+    return ws_record_failure(WS_EUNSUPPORTED, "evict: 2^24 requests times heads or more");
   if (e->to && (e->to_stride < 0 || (int64_t)e->to_cols * c->page_size < e->keep))
     return invalid("evict: the kept rows need pages to go to");
   return WS_OK;

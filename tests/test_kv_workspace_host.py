@@ -89,3 +89,14 @@ def test_a_workspace_that_is_too_small():
 
     assert weigh(at * 7, n - 4) == B.WS_EWORKSPACE and weigh(None, n) == B.WS_EWORKSPACE
     assert weigh(at * 7 + 2, n) == B.WS_EINVAL
+
+
+def test_more_requests_and_heads_than_a_launch_has():
+    """Refused before sizes are multiplied that 64 bits do not hold."""
+    n = ctypes.c_size_t(7)
+    for n_seq, heads in ((1 << 24, 1), (1 << 19, 32), ((1 << 31) - 1, 1 << 30)):
+        rc = kv._lib().wait_kv_evict_workspace_bytes(cache(kv_heads=heads, pages=1, page_size=1),
+                                                     eviction(n_seq=n_seq, table_cols=1 << 17, max_kv_len=1 << 17),
+                                                     ctypes.byref(n))
+        assert rc == B.WS_EUNSUPPORTED and n.value == 7
+    assert evict_bytes((1 << 24) - 1, 1, 1 << 17) == 0
