@@ -328,7 +328,10 @@ __global__ void __launch_bounds__(256) norm_kernel(Args a) {
 }
 
 // Any alignment, any even part: a wave takes one vector, a lane its pairs, one at
-// a time, each element in one lane only, so that out may be x.
+// a time, each element in one lane only, so that out may be x.  Bound by instructions,
+// an element a load and the vector read twice: 8192 x 32 vectors of 128 bf16 at odd
+// addresses 109 us (22 with aligned ones), with 66 elements turned 134; 8191 tokens of
+// 32 + 2 x 8 heads at odd addresses, fp16 into int8, 236 (34).
 template <class T, int TYPE>
 __global__ void __launch_bounds__(256) norm_single_kernel(Args a) {
   using raw = typename T::raw;

@@ -104,7 +104,8 @@ __device__ __forceinline__ float old_weight(const Args &a, const Seq &s, int32_t
 // products have taken the last; more rows go over the same keys again.  128
 // requests of 513 to 1512 keys, 32 heads of 128: fp8 (591 MB) 127 us (4.7 TB/s; 111
 // without writing the weights, whose 64 bytes a page and head are half lines),
-// bf16 (1.1 GB) 222 us (5.0 TB/s).  Half the keys at a time took 162 us, two sets
+// bf16 (1.1 GB) 222 us (5.0 TB/s).  All keys are read, also where a window leaves few
+// of them: one token over 131,072 keys takes 30 us with a window of 257 as without.  Half the keys at a time took 162 us, two sets
 // of registers for the keys 146: fewer waves then hide the memory's latency.
 
 constexpr int kFewRows = 16;
@@ -277,10 +278,12 @@ __device__ __forceinline__ void few_rows(const Args &a, int32_t id) {  // of a w
 // rows are split over workgroups too and a second kernel adds the parts in their
 // order.
 //
-// Two prompts of 6011 and 8192 over 32 heads of 128 bf16 (324 GFLOP): 365 to 380 us
+// Two prompts of 6011 and 8192 over 32 heads of 128 bf16 (324 GFLOP): 363 to 384 us
 // between cards, 0.87 PFLOP/s, 63 % of what a library product of 8192^3 reaches here.
-// Of its 361 us in one run the products without the exponentials took 294, and all
-// but the copies 310: neither hides wholly behind the others.  32 keys a wave and
+// No unit is full: matrix units are busy 40 % of the time, vector units 56 %, and a
+// quarter of the waves' cycles are waits; both units' work in one loop by itself would
+// take 193 us.  Of 361 us in one run the products without the exponentials took 294,
+// and all but the copies 310: neither hides wholly behind the others.  32 keys a wave and
 // three workgroups a CU took 416 us, eight waves that share the copies 404.  The last
 // 32 of 131,072 tokens, 64 heads on 8, int8: 110 us, four blocks of rows for each 256
 // keys behind a start of several us; keeping the rows in shared memory from one tile
@@ -628,7 +631,8 @@ __device__ __forceinline__ void many_rows(const Args &a, int32_t id, char *smem)
     const bool has = key < end && lane < own;
     if (__any(has && row_at != kNoRow && total != total)) {
       // Again, rows that saw nothing left out by a choice, by the wave alone.  A choice
-      // in the loop above took 3 to 5 % more of everything.
+      // in the loop above took 3 to 5 % more of everything; here a key that is NaN to
+      // rows that see it takes its wave up to four times as long.
       float again[M::ktiles][2] = {};
       for (int32_t r0 = max(some.lo, lo) / 32 * 32; r0 < some.hi; r0 += 32) {
         const int32_t row = min(r0 + n32, rows - 1), token = row / a.group;
@@ -756,13 +760,13 @@ Layout layout_of(const ws_kv_cache &c, const ws_kv_batch &b) {
   // Parts of a 1024th of the batch's blocks of rows against tiles of keys, four
   // workgroups a CU (causal, half of it is work); the rows are those that there are,
   // however many requests have few of them.  One prompt of 8192 over 16 heads on one KV
-  // head: 222 us, 274 with half as many parts, 439 with a quarter.  A prompt of 512
-  // behind 1024 keys beside 31 single tokens, 32 heads on 8: 32 us, 73 with as many
+  // head: 205 us, 276 with half as many parts, 438 with a quarter.  A prompt of 512
+  // behind 1024 keys beside 31 single tokens, 32 heads on 8: 34 us, 73 with as many
   // parts for each request as for the longest, most of them empty.
   // A part has four blocks at least, where joining costs what it saves: the last 32 of
   // 8192 tokens, 64 heads on 8, 17 us, 24 with two; two where there would be a
-  // workgroup for half of the CUs at most: 63 tokens, 128 heads on 8, D = 64, 11.4 us,
-  // 15.3 with four.  Up to 64 MB of sums.
+  // workgroup for half of the CUs at most: 63 tokens, 128 heads on 8, D = 64, 11.8 us,
+  // 16.1 with four.  Up to 64 MB of sums.
   const int64_t block = c.dim == 256 ? 32 : 64, all_rows = (int64_t)b.n_tokens * group;
   const int64_t tiles = (int64_t)c.kv_heads * L.tiles;
   const int64_t keys = tiles * many_keys(c.dim) * 4;  // sums of a part

@@ -338,7 +338,9 @@ def evict(cache: Cache, pages: torch.Tensor, kv_lens: torch.Tensor, weights: tor
     the kept ones stay as they are; pages of ``pages`` behind them are free.
 
     ``pages``, ``to`` and ``kv_lens`` are int32 and stay on the device;
-    ``max_kv_len`` bounds the lengths for the launch's layout.  Requests share no
+    ``max_kv_len`` bounds the lengths for the launch's layout (by default the width
+    of ``pages``; far above the lengths it costs time and workspace).  Keys and
+    values, weights and arguments share no memory.  Requests share no
     pages, and all of their pages are there (include/wait_kv_budget.h).  Returns
     (kept [requests, kv_heads, keep] int32, the indices of the kept keys, -1
     behind a request's last; new lengths [requests], min(kv_lens, keep)).  Attention over the
