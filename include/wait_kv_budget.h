@@ -49,10 +49,10 @@ int wait_kv_weigh(const ws_kv_cache *cache, const ws_kv_batch *batch, const ws_k
  * weights go to offset d % page_size of page to[b * to_stride + d / page_size],
  * or of the request's own pages where `to` is NULL.  Rows behind them stay as
  * they are.
- * Requests share no pages, and pages of `to` are no request's.  Pages are there:
- * of a row whose page is outside 0 .. pages-1 nothing is read, its weight is
- * less than all others, and nothing is written in its place; keys behind the
- * table's columns do not count. */
+ * Requests share no pages, and pages of `to` are no request's (`to` is not `table`).
+ * Pages are there: of a row whose page is outside 0 .. pages-1 nothing is read, its
+ * weight is less than all others, and nothing is written in its place; keys behind
+ * the table's columns do not count. */
 typedef struct {
   const int32_t *table;
   int64_t table_stride;

@@ -689,6 +689,7 @@ int wait_kv_evict(const ws_kv_cache *cache, const ws_kv_eviction *eviction, floa
       return invalid("evict: weights and outputs must not overlap the cache or one another");
     if (shares(space, in_cache) || shares(space, {w, list, lens, read[0], read[1], read[2]}))
       return invalid("evict: the workspace must be its own memory");
+    if (e.to && e.to == e.table) return invalid("evict: the requests' own pages are no others: leave `to` out");
     if (!e.to && (shares(in_cache.k, in_cache.v) || shares(in_cache.ks, in_cache.vs)))
       return invalid("evict: keys and values that move in place must not overlap");
     Args a{};

@@ -84,6 +84,12 @@ def test_keys_and_values_of_one_place():
     refused(evict(eight(v_scale=KS)))
 
 
+def test_an_eviction_to_the_requests_own_pages():
+    """Rows on their way to other pages do not wait for one another."""
+    refused(evict(sixteen(), to=TABLE), "own pages")
+    refused(evict(sixteen(), to=TABLE, to_stride=8, to_cols=8), "own pages")
+
+
 def test_queries_that_enter_the_cache():
     q, k, v = (rows(data=Q + 128 * i, token=512) for i in (0, 4, 6))
 
